@@ -299,6 +299,50 @@ int peagle_layer_partitioned(peagle_ctx *ctx, const peagle_problem_t *prob,
                              float *LSE, void *dX, void *dW, void *stream);
 
 /*
+ * Operators around the drafter layer in a training or scoring program: the norm in front of the
+ * projections, the log probabilities of drafted tokens, the optimizer.  (The paper trains with them
+ * and does not describe them.)  They differ from the attention calls in three ways:
+ *   - element types are an argument (peagle_dtype); sums and statistics are fp32;
+ *   - rows may lie apart: a leading dimension (elements from one row to the next, at least the row's
+ *     length) goes with every matrix, and any base address that is a multiple of the element size is
+ *     taken (16-byte aligned rows are faster);
+ *   - the device that was current before the call is current after it, and scratch that a call
+ *     keeps in the context stays where it is until peagle_destroy, so calls may be captured into CUDA
+ *     graphs, the first one too.  Calls that overlap on the GPU still need a context each.
+ * rows == 0 (tensors of 0 elements) returns PEAGLE_OK and changes nothing.  Outputs must not overlap
+ * inputs or each other, except where "in place" is stated.
+ */
+typedef enum peagle_dtype { PEAGLE_F32 = 0, PEAGLE_BF16 = 1 } peagle_dtype;
+
+/*
+ * Layer norm and RMS norm of rows (Section 2: a LLaMA-3-style layer).  With mu = mean of the row
+ * (PEAGLE_NORM_LAYER) or 0 (PEAGLE_NORM_RMS):
+ *     rstd = 1 / sqrt(mean((x - mu)^2) + eps),   y = (x - mu) * rstd * weight + bias
+ * X, Y are dev [rows][cols] of x_dtype; weight, bias dev [cols] of w_dtype, each may be NULL (1 and 0).
+ * mean, rstd are dev fp32 [rows], what the backward needs; each may be NULL (mean is not written by
+ * PEAGLE_NORM_RMS).  eps > 0.  In place: Y may be X with the same leading dimension.  A NaN or infinity
+ * stays in its row.  Asynchronous.
+ */
+typedef enum peagle_norm { PEAGLE_NORM_LAYER = 0, PEAGLE_NORM_RMS = 1 } peagle_norm;
+int peagle_norm_fwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
+                    int32_t cols, const void *X, int64_t ldx, const void *weight, const void *bias,
+                    float eps, void *Y, int64_t ldy, float *mean, float *rstd, void *stream);
+
+/*
+ * Its backward.  With xh = (x - mean) * rstd and u = dy * weight:
+ *     dx = rstd * (u - mean_row(u) - xh * mean_row(u * xh))      (no mean_row(u) for PEAGLE_NORM_RMS)
+ *     dweight_acc[c] += sum over rows of dy * xh,   dbias_acc[c] += sum over rows of dy     (ADDED)
+ * X and weight as in the forward, mean (PEAGLE_NORM_LAYER only) and rstd its outputs; dY, dX dev
+ * [rows][cols] of x_dtype.  dweight_acc, dbias_acc dev fp32 [cols], zeroed by the caller once per
+ * accumulation; each may be NULL.  The sums have a fixed order and repeat bit for bit.  In place: dX may
+ * be dY or X with the same leading dimension.  Scratch in the context.  Asynchronous.
+ */
+int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
+                    int32_t cols, const void *X, int64_t ldx, const void *weight, const float *mean,
+                    const float *rstd, const void *dY, int64_t lddy, void *dX, int64_t lddx,
+                    float *dweight_acc, float *dbias_acc, void *stream);
+
+/*
  * Algorithm 1, host only: segment of every token.  `boundaries` is host [S+1], context-token
  * positions with boundaries[0]=0 and boundaries[S]=n (Algorithm 1's B).  Depth 0 and 1 tokens
  * go by their position anchor+depth (a position at or beyond n stays in the last segment);

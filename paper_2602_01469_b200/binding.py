@@ -28,7 +28,10 @@ EXPORTS = [
     "peagle_timing_enable", "peagle_timing_read", "peagle_attn_fwd_static",
     "peagle_rope_qkv_fwd", "peagle_rope_qkv_bwd", "peagle_attn_partitioned_acc", "peagle_cast_grads",
     "peagle_gemm_bf16", "peagle_layer_partitioned", "peagle_selftest_wait_expiry",
+    "peagle_norm_fwd", "peagle_norm_bwd",
 ]
+
+NORM = {"layer": 0, "rms": 1}  # peagle_norm
 
 
 class peagle_range_t(ctypes.Structure):
@@ -111,6 +114,46 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
+def _stream_on(ctx, stream):
+    """Like ``_stream``; without one, the current stream of the context's own device."""
+    if stream is None:
+        import torch
+        return ctypes.c_void_p(torch.cuda.current_stream(ctx.device).cuda_stream)
+    return _stream(stream)
+
+
+def _dtype(t):
+    """peagle_dtype of a tensor."""
+    import torch
+    if t.dtype == torch.float32:
+        return 0
+    if t.dtype == torch.bfloat16:
+        return 1
+    raise PeagleError(STATUS["BAD_SHAPE"])
+
+
+def _require(ok, status="BAD_SHAPE"):
+    if not ok:
+        raise PeagleError(STATUS[status])
+
+
+def _on(ctx, *tensors):
+    """Every tensor that is given lies on the context's device."""
+    for t in tensors:
+        _require(t is None or (t.is_cuda and t.device.index == ctx.device))
+
+
+def _ld(t, rows, cols):
+    """Leading dimension of a [rows, cols] tensor whose rows are contiguous."""
+    _require(t.dim() == 2 and tuple(t.shape) == (rows, cols) and (cols == 1 or t.stride(1) == 1))
+    return ctypes.c_int64(max(t.stride(0), cols) if rows == 1 else t.stride(0))
+
+
+def _vector(t, n, *dtypes):
+    """A contiguous vector of n elements, or none."""
+    _require(t is None or (t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1) and t.dtype in dtypes))
+
+
 class Problem:
     """Owns the host arrays a peagle_problem_t points to."""
 
@@ -151,6 +194,7 @@ def _partition_array(parts):
 class Context:
     def __init__(self, device: int = 0):
         self.h = ctypes.c_void_p()
+        self.device = int(device)
         _check(lib().peagle_create(ctypes.byref(self.h), int(device)))
 
     def close(self):
@@ -271,6 +315,42 @@ def peagle_layer_partitioned(ctx, prob: Problem, parts, X, W, rope_base, dO, O, 
     _check(lib().peagle_layer_partitioned(ctx.h, prob.ref(), arr, len(parts), _ptr(X), _ptr(W),
                                           int(X.shape[1]), ctypes.c_float(rope_base), _ptr(dO), _ptr(O),
                                           _ptr(LSE), _ptr(dX), _ptr(dW), _stream(stream)), ctx.h)
+
+
+def peagle_norm_fwd(ctx, kind, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
+    """Layer norm (``NORM["layer"]``) or RMS norm (``NORM["rms"]``) of the rows of X into Y; weight, bias, and
+    the fp32 statistics mean and rstd may be None.  Device tensors; rows of X and Y may lie apart."""
+    import torch
+    _require(X.dim() == 2)
+    rows, cols = X.shape
+    w = weight if weight is not None else bias
+    _require(Y.dtype == X.dtype and (weight is None or bias is None or weight.dtype == bias.dtype))
+    for t in (weight, bias):
+        _vector(t, cols, torch.float32, torch.bfloat16)
+    for t in (mean, rstd):
+        _vector(t, rows, torch.float32)
+    _on(ctx, X, weight, bias, Y, mean, rstd)
+    _check(lib().peagle_norm_fwd(ctx.h, int(kind), _dtype(X), _dtype(w) if w is not None else 0, int(rows), int(cols),
+                                 _ptr(X), _ld(X, rows, cols), _ptr(weight), _ptr(bias), ctypes.c_float(eps), _ptr(Y),
+                                 _ld(Y, rows, cols), _ptr(mean), _ptr(rstd), _stream_on(ctx, stream)), ctx.h)
+
+
+def peagle_norm_bwd(ctx, kind, X, weight, mean, rstd, dY, dX, dweight_acc=None, dbias_acc=None, stream=None):
+    """Backward of the norm: dX, and the gradients of weight and bias ADDED to fp32 sums."""
+    import torch
+    _require(X.dim() == 2)
+    rows, cols = X.shape
+    _require(dY.dtype == X.dtype and dX.dtype == X.dtype)
+    _vector(weight, cols, torch.float32, torch.bfloat16)
+    for t in (mean, rstd):
+        _vector(t, rows, torch.float32)
+    for t in (dweight_acc, dbias_acc):
+        _vector(t, cols, torch.float32)
+    _on(ctx, X, weight, mean, rstd, dY, dX, dweight_acc, dbias_acc)
+    _check(lib().peagle_norm_bwd(ctx.h, int(kind), _dtype(X), _dtype(weight) if weight is not None else 0, int(rows),
+                                 int(cols), _ptr(X), _ld(X, rows, cols), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dY),
+                                 _ld(dY, rows, cols), _ptr(dX), _ld(dX, rows, cols), _ptr(dweight_acc), _ptr(dbias_acc),
+                                 _stream_on(ctx, stream)), ctx.h)
 
 
 def peagle_selftest_wait_expiry(ctx, limit_ms: int = 20, stream=None):

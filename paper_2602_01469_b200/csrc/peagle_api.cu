@@ -22,6 +22,9 @@ struct peagle_ctx {
     EncodeTiledFn encode = nullptr;
     int *status = nullptr; // device status word
     DevBuf plan_buf, bwd_buf, acc_buf, host_buf, layer_buf;
+    DevBuf norm_buf;
+    DevBuf kept[48]; // outgrown scratch that a captured graph may still point to; at least doubles each time
+    int n_kept = 0;
     int64_t launches = 0;
     char cuda_err[256] = {0};
     bool timing = false;
@@ -77,6 +80,49 @@ int ensure(peagle_ctx *ctx, DevBuf &b, size_t bytes, cudaStream_t s)
     b.bytes = want;
     return PEAGLE_OK;
 }
+
+// Grows a scratch buffer that captured graphs may point to: the old one is kept until the context is
+// destroyed (each is at least twice the last, so together they are no more than the largest).  Allocating
+// is allowed while a stream is captured, here or in another thread, in the relaxed mode.
+int ensure_kept(peagle_ctx *ctx, DevBuf &b, size_t bytes)
+{
+    if (bytes <= b.bytes)
+        return PEAGLE_OK;
+    if (b.ptr && ctx->n_kept == (int)(sizeof(ctx->kept) / sizeof(ctx->kept[0])))
+        return PEAGLE_ERR_WORKSPACE;
+    const size_t want = std::max(bytes + 4096, 2 * b.bytes);
+    void *p = nullptr;
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    const cudaError_t e = cudaMalloc(&p, want);
+    cudaThreadExchangeStreamCaptureMode(&mode);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return PEAGLE_ERR_WORKSPACE;
+    }
+    if (b.ptr)
+        ctx->kept[ctx->n_kept++] = b;
+    b.ptr = p;
+    b.bytes = want;
+    return PEAGLE_OK;
+}
+
+// Makes a device current for the length of a call.
+struct OnDevice {
+    int before = -1, device;
+    cudaError_t error;
+    explicit OnDevice(int d) : device(d)
+    {
+        error = cudaGetDevice(&before);
+        if (error == cudaSuccess && before != d)
+            error = cudaSetDevice(d);
+    }
+    ~OnDevice()
+    {
+        if (before >= 0 && before != device)
+            cudaSetDevice(before);
+    }
+};
 
 // Next (start, stop) event pair of a kind, or nulls when timing is off or the pool is full.
 void next_events(peagle_ctx *ctx, int kind, cudaEvent_t *e0, cudaEvent_t *e1)
@@ -443,10 +489,13 @@ int peagle_destroy(peagle_ctx *ctx)
         return PEAGLE_ERR_NULL;
     cudaSetDevice(ctx->device);
     cudaDeviceSynchronize();
-    DevBuf *bufs[5] = {&ctx->plan_buf, &ctx->bwd_buf, &ctx->acc_buf, &ctx->host_buf, &ctx->layer_buf};
+    DevBuf *bufs[6] = {&ctx->plan_buf, &ctx->bwd_buf,   &ctx->acc_buf,
+                       &ctx->host_buf, &ctx->layer_buf, &ctx->norm_buf};
     for (DevBuf *b : bufs)
         if (b->ptr)
             cudaFree(b->ptr);
+    for (int i = 0; i < ctx->n_kept; ++i)
+        cudaFree(ctx->kept[i].ptr);
     if (ctx->status)
         cudaFree(ctx->status);
     for (int k = 0; k < 2; ++k)
@@ -1198,6 +1247,109 @@ int peagle_attn_partitioned_host(peagle_ctx *ctx, const peagle_problem_t *prob,
         CKD(cudaStreamSynchronize(st));
     return PEAGLE_OK;
 #undef CKD
+}
+
+// ---- operators around the layer: norm
+
+static size_t dtype_size(int32_t dtype) { return dtype == PEAGLE_F32 ? 4 : dtype == PEAGLE_BF16 ? 2 : 0; }
+static bool aligned_to(const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+static int norm_args_ok(const NormArgs &a)
+{
+    if ((a.kind != PEAGLE_NORM_LAYER && a.kind != PEAGLE_NORM_RMS) || !dtype_size(a.x_dtype) ||
+        !dtype_size(a.w_dtype) || a.rows < 0 || a.cols < 1)
+        return PEAGLE_ERR_BAD_SHAPE;
+    return PEAGLE_OK;
+}
+
+int peagle_norm_fwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
+                    int32_t cols, const void *X, int64_t ldx, const void *weight, const void *bias,
+                    float eps, void *Y, int64_t ldy, float *mean, float *rstd, void *stream)
+{
+    if (!ctx)
+        return PEAGLE_ERR_NULL;
+    NormArgs a = {};
+    a.kind = kind;
+    a.x_dtype = x_dtype;
+    a.w_dtype = w_dtype;
+    a.rows = rows;
+    a.cols = cols;
+    const int rc = norm_args_ok(a);
+    if (rc != PEAGLE_OK)
+        return rc;
+    if (!(eps > 0.f) || ldx < cols || ldy < cols)
+        return PEAGLE_ERR_BAD_SHAPE;
+    if (rows == 0)
+        return PEAGLE_OK;
+    if (!X || !Y)
+        return PEAGLE_ERR_NULL;
+    const size_t xs = dtype_size(x_dtype), ws = dtype_size(w_dtype);
+    if (!aligned_to(X, xs) || !aligned_to(Y, xs) || !aligned_to(weight, ws) || !aligned_to(bias, ws) ||
+        !aligned_to(mean, 4) || !aligned_to(rstd, 4))
+        return PEAGLE_ERR_ALIGN;
+    a.X = X;
+    a.ldx = ldx;
+    a.weight = weight;
+    a.bias = bias;
+    a.eps = eps;
+    a.Y = Y;
+    a.ldy = ldy;
+    a.mean = kind == PEAGLE_NORM_LAYER ? mean : nullptr;
+    a.rstd = rstd;
+    const OnDevice on(ctx->device);
+    CK(on.error);
+    ctx->launches += launch_norm_fwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    CK(cudaGetLastError());
+    return PEAGLE_OK;
+}
+
+int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
+                    int32_t cols, const void *X, int64_t ldx, const void *weight, const float *mean,
+                    const float *rstd, const void *dY, int64_t lddy, void *dX, int64_t lddx,
+                    float *dweight_acc, float *dbias_acc, void *stream)
+{
+    if (!ctx)
+        return PEAGLE_ERR_NULL;
+    NormArgs a = {};
+    a.kind = kind;
+    a.x_dtype = x_dtype;
+    a.w_dtype = w_dtype;
+    a.rows = rows;
+    a.cols = cols;
+    int rc = norm_args_ok(a);
+    if (rc != PEAGLE_OK)
+        return rc;
+    if (ldx < cols || lddy < cols || lddx < cols)
+        return PEAGLE_ERR_BAD_SHAPE;
+    if (rows == 0)
+        return PEAGLE_OK;
+    if (!X || !rstd || !dY || !dX || (kind == PEAGLE_NORM_LAYER && !mean))
+        return PEAGLE_ERR_NULL;
+    const size_t xs = dtype_size(x_dtype);
+    if (!aligned_to(X, xs) || !aligned_to(dY, xs) || !aligned_to(dX, xs) ||
+        !aligned_to(weight, dtype_size(w_dtype)) || !aligned_to(mean, 4) || !aligned_to(rstd, 4) ||
+        !aligned_to(dweight_acc, 4) || !aligned_to(dbias_acc, 4))
+        return PEAGLE_ERR_ALIGN;
+    a.X = X;
+    a.ldx = ldx;
+    a.weight = weight;
+    a.mean_in = kind == PEAGLE_NORM_LAYER ? mean : nullptr;
+    a.rstd_in = rstd;
+    a.dY = dY;
+    a.lddy = lddy;
+    a.dX = dX;
+    a.lddx = lddx;
+    a.dw = dweight_acc;
+    a.db = dbias_acc;
+    const OnDevice on(ctx->device);
+    CK(on.error);
+    rc = ensure_kept(ctx, ctx->norm_buf, norm_bwd_scratch(a, ctx->n_sm));
+    if (rc != PEAGLE_OK)
+        return rc;
+    a.partial = static_cast<float *>(ctx->norm_buf.ptr);
+    ctx->launches += launch_norm_bwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    CK(cudaGetLastError());
+    return PEAGLE_OK;
 }
 
 int peagle_assign_segments(const int32_t *anchor, const int32_t *depth, int32_t count, int32_t K,

@@ -202,6 +202,28 @@ int launch_gemm(EncodeTiledFn enc, const void *A, long long lda, int a_t, const 
                 int b_t, void *C, long long ldc, int c_f32_add, int M, int N, int K, int *status,
                 cudaStream_t s);
 
+// Layer norm / RMS norm (peagle_norm.cu).  Row strides in elements.
+struct NormArgs {
+    int kind, x_dtype, w_dtype, rows, cols;
+    const void *X;
+    int64_t ldx;
+    const void *weight, *bias; // may be null
+    float eps;
+    void *Y; // forward
+    int64_t ldy;
+    float *mean, *rstd;
+    const float *mean_in, *rstd_in; // backward
+    const void *dY;
+    int64_t lddy;
+    void *dX;
+    int64_t lddx;
+    float *dw, *db;   // added to; may be null
+    float *partial;   // backward: norm_bwd_scratch() bytes
+};
+int launch_norm_fwd(const NormArgs &a, int n_sm, cudaStream_t s);
+size_t norm_bwd_scratch(const NormArgs &a, int n_sm);
+int launch_norm_bwd(const NormArgs &a, int n_sm, cudaStream_t s);
+
 // Packed-metadata form of the attention predicate: m = anchor << 8 | depth.
 // (depth_k == 0 and anchor_k <= anchor_q) or (anchor_k == anchor_q and depth_k <= depth_q)
 __host__ __device__ inline bool allowed_packed(int32_t mq, int32_t mk)

@@ -1,0 +1,115 @@
+"""CPU pins of the fp64 definitions of the operators around the layer: closed forms, torch's own
+operators and autograd, central differences; and the refusals that the library makes on the host."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops_oracle as oo
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("affine", [True, False])
+def test_norm_equals_torch_and_its_autograd(kind, affine):
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(5, 23, generator=gen, dtype=torch.float64, requires_grad=True)
+    w = torch.randn(23, generator=gen, dtype=torch.float64, requires_grad=True) if affine else None
+    b = torch.randn(23, generator=gen, dtype=torch.float64, requires_grad=True) if affine and kind == "layer" else None
+    dy = torch.randn(5, 23, generator=gen, dtype=torch.float64)
+    if kind == "layer":
+        y = torch.nn.functional.layer_norm(x, (23,), w, b, 1e-3)
+    else:
+        y = torch.nn.functional.rms_norm(x, (23,), w, 1e-3)
+    (y * dy).sum().backward()
+    num = lambda t: None if t is None else t.detach().numpy()
+    got, mean, rstd = oo.norm_fwd(kind, num(x), num(w), num(b), 1e-3)
+    assert np.allclose(got, num(y), atol=1e-13)
+    dx, dw, db = oo.norm_bwd(kind, num(x), num(w), mean, rstd, dy.numpy())
+    assert np.allclose(dx, x.grad.numpy(), atol=1e-13)
+    if affine:
+        assert np.allclose(dw, w.grad.numpy(), atol=1e-13)
+    if b is not None:
+        assert np.allclose(db, b.grad.numpy(), atol=1e-13)
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+def test_norm_gradients_by_central_differences(kind):
+    rng = np.random.default_rng(1)
+    x, w, dy = rng.standard_normal((3, 7)), rng.standard_normal(7), rng.standard_normal((3, 7))
+
+    def loss(x, w):
+        return float((oo.norm_fwd(kind, x, w, None, 0.1)[0] * dy).sum())
+
+    _, mean, rstd = oo.norm_fwd(kind, x, w, None, 0.1)
+    dx, dw, _ = oo.norm_bwd(kind, x, w, mean, rstd, dy)
+    h = 1e-5
+    for i in np.ndindex(3, 7):
+        up, dn = x.copy(), x.copy()
+        up[i] += h
+        dn[i] -= h
+        assert (loss(up, w) - loss(dn, w)) / (2 * h) == pytest.approx(dx[i], rel=1e-6, abs=1e-8)
+    for i in range(7):
+        up, dn = w.copy(), w.copy()
+        up[i] += h
+        dn[i] -= h
+        assert (loss(x, up) - loss(x, dn)) / (2 * h) == pytest.approx(dw[i], rel=1e-6, abs=1e-8)
+
+
+def test_norm_closed_forms():
+    y, mean, rstd = oo.norm_fwd("layer", [[3.0, 1.0]], [2.0, 2.0], [0.5, 0.5], 0.0)
+    assert np.allclose(y, [[2.5, -1.5]]) and np.allclose(mean, [2.0]) and np.allclose(rstd, [1.0])
+    y, _, rstd = oo.norm_fwd("rms", [[3.0, 4.0]], None, None, 0.0)
+    assert np.allclose(rstd, [1 / np.sqrt(12.5)]) and np.allclose(y, np.array([[3.0, 4.0]]) / np.sqrt(12.5))
+
+
+# ------------------------------------------------------------------ refusals, before any device is touched
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2602_01469_b200 import binding, build
+    build.build()
+    return binding.lib()
+
+
+@pytest.fixture(scope="module")
+def zeros():
+    """Stands in for a context: the calls below are refused, or have nothing to do, before they look into it."""
+    import ctypes
+    return ctypes.create_string_buffer(1 << 16)
+
+
+def _norm_call(lib, ctx, back, **over):
+    import ctypes
+    a = dict(kind=1, x_dtype=1, w_dtype=1, rows=4, cols=64, X=4096, ldx=64, weight=0, bias=0, eps=1e-5, Y=8192, ldy=64,
+             mean=0, rstd=12288, dY=16384, lddy=64)
+    a.update(over)
+    i32, i64, ptr = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+    head = [ctx, i32(a["kind"]), i32(a["x_dtype"]), i32(a["w_dtype"]), i32(a["rows"]), i32(a["cols"]), ptr(a["X"]),
+            i64(a["ldx"]), ptr(a["weight"])]
+    if back:
+        return lib.peagle_norm_bwd(*head, ptr(a["mean"]), ptr(a["rstd"]), ptr(a["dY"]), i64(a["lddy"]), ptr(a["Y"]),
+                                   i64(a["ldy"]), ptr(0), ptr(0), ptr(0))
+    return lib.peagle_norm_fwd(*head, ptr(a["bias"]), ctypes.c_float(a["eps"]), ptr(a["Y"]), i64(a["ldy"]), ptr(a["mean"]),
+                               ptr(a["rstd"]), ptr(0))
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("over,status", [
+    ({"rows": 0}, "OK"), ({"rows": -1}, "BAD_SHAPE"), ({"cols": 0}, "BAD_SHAPE"), ({"kind": 2}, "BAD_SHAPE"),
+    ({"kind": -1}, "BAD_SHAPE"), ({"x_dtype": 2}, "BAD_SHAPE"), ({"w_dtype": -1}, "BAD_SHAPE"), ({"ldx": 63}, "BAD_SHAPE"),
+    ({"ldy": 63}, "BAD_SHAPE"), ({"X": 0}, "NULL"), ({"Y": 0}, "NULL"), ({"X": 4097}, "ALIGN"), ({"Y": 8193}, "ALIGN"),
+    ({"x_dtype": 0, "X": 4098}, "ALIGN"), ({"weight": 4097}, "ALIGN"), ({"rstd": 12290}, "ALIGN"),
+])
+def test_norm_refusals(lib, zeros, back, over, status):
+    from paper_2602_01469_b200 import binding
+    assert _norm_call(lib, zeros, back, **over) == binding.STATUS[status]
+
+
+def test_norm_refusals_of_one_direction(lib, zeros):
+    from paper_2602_01469_b200 import binding
+    S = binding.STATUS
+    for eps in (0.0, -1e-5, float("nan")):
+        assert _norm_call(lib, zeros, False, eps=eps) == S["BAD_SHAPE"]
+    assert _norm_call(lib, zeros, True, kind=0) == S["NULL"]          # layer norm without its mean
+    assert _norm_call(lib, zeros, True, rstd=0) == S["NULL"]
+    assert _norm_call(lib, zeros, True, dY=0) == S["NULL"]
+    assert _norm_call(lib, zeros, True, lddy=10) == S["BAD_SHAPE"]
+    assert _norm_call(lib, None, False) == _norm_call(lib, None, True) == S["NULL"]
