@@ -343,6 +343,45 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
                     float *dweight_acc, float *dbias_acc, void *stream);
 
 /*
+ * Log probabilities of given tokens, with entropy and top alternatives: the loss on the drafted tokens
+ * (Section 2: the drafter predicts K tokens at once), or the scores of a served request.  With
+ * s_j = scale * logits[r][j] (0 < scale <= 1e20, an inverse temperature):
+ *     lse = log sum_j exp(s_j),  logprob = s_token - lse,  entropy = -sum_j p_j log p_j,  p_j = exp(s_j - lse)
+ * and, of the top_k largest logits, top_ids (larger logit first, of equal ones the lower id first; -0 equals
+ * 0) and top_logprobs = s_id - lse.  logits is dev [rows][vocab] of `dtype`; tokens dev int32 [rows], -1
+ * where a row has no token: its logprob is 0, all else as for any row.  logprob, lse, entropy are dev fp32
+ * [rows], top_logprobs fp32 and top_ids int32 [rows][top_k] (contiguous); each may be NULL, tokens too when
+ * logprob is.  0 <= top_k <= min(vocab, PEAGLE_MAX_TOP_K), and the two top outputs are either both there or
+ * both NULL (top_k == 0).  -inf is a token of probability zero, and
+ *   - a row of nothing but -inf (or logits that scale takes there) has lse = logprob = -inf, entropy 0, top
+ *     ids 0, 1, .. with log probability -inf;
+ *   - a row with a NaN or +inf has NaN in all its fp32 outputs (0 for the logprob of token -1), top ids -1;
+ *   - a token outside [-1, vocab) gets logprob NaN and sets PEAGLE_ERR_BAD_META in the status word.
+ * Nothing depends on the order in which blocks finish.  Asynchronous.
+ */
+#define PEAGLE_MAX_TOP_K 64
+int peagle_token_logprobs_fwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
+                              const void *logits, int64_t ld, const int32_t *tokens, float scale,
+                              float *logprob, float *lse, float *entropy, int32_t top_k,
+                              float *top_logprobs, int32_t *top_ids, void *stream);
+
+/*
+ * Its backward: the gradient of the logits for gradients g_logprob, g_entropy (dev fp32 [rows], either may
+ * be NULL: zero) that reach logprob and entropy.  With log p_j = s_j - lse:
+ *     dlogits[r][j] = scale * ( g_logprob ([j = token] - p_j) - g_entropy p_j (log p_j + entropy) )
+ * where g_logprob counts as zero in a row whose token is -1 (or outside the vocabulary: the forward has
+ * reported it).  lse, and entropy when g_entropy is given, are the forward's.  (An lse of 8192 or more in
+ * magnitude, a row of the type's lowest number for one, has too few digits after the point in fp32: such a row
+ * is read once more for its maximum and sum.)  A row of nothing but -inf gets zeros, a row with NaN or +inf
+ * NaN; a row whose two gradients are zero gets zeros whatever its logits are, and they are not read.  In
+ * place: dlogits may be logits with the same leading dimension.  Asynchronous.
+ */
+int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
+                              const void *logits, int64_t ld, const int32_t *tokens, float scale,
+                              const float *lse, const float *entropy, const float *g_logprob,
+                              const float *g_entropy, void *dlogits, int64_t ldd, void *stream);
+
+/*
  * Algorithm 1, host only: segment of every token.  `boundaries` is host [S+1], context-token
  * positions with boundaries[0]=0 and boundaries[S]=n (Algorithm 1's B).  Depth 0 and 1 tokens
  * go by their position anchor+depth (a position at or beyond n stays in the last segment);

@@ -28,7 +28,7 @@ EXPORTS = [
     "peagle_timing_enable", "peagle_timing_read", "peagle_attn_fwd_static",
     "peagle_rope_qkv_fwd", "peagle_rope_qkv_bwd", "peagle_attn_partitioned_acc", "peagle_cast_grads",
     "peagle_gemm_bf16", "peagle_layer_partitioned", "peagle_selftest_wait_expiry",
-    "peagle_norm_fwd", "peagle_norm_bwd",
+    "peagle_norm_fwd", "peagle_norm_bwd", "peagle_token_logprobs_fwd", "peagle_token_logprobs_bwd",
 ]
 
 NORM = {"layer": 0, "rms": 1}  # peagle_norm
@@ -351,6 +351,46 @@ def peagle_norm_bwd(ctx, kind, X, weight, mean, rstd, dY, dX, dweight_acc=None, 
                                  int(cols), _ptr(X), _ld(X, rows, cols), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dY),
                                  _ld(dY, rows, cols), _ptr(dX), _ld(dX, rows, cols), _ptr(dweight_acc), _ptr(dbias_acc),
                                  _stream_on(ctx, stream)), ctx.h)
+
+
+def peagle_token_logprobs_fwd(ctx, logits, tokens, scale=1.0, logprob=None, lse=None, entropy=None, top_logprobs=None,
+                              top_ids=None, stream=None):
+    """Log probability of ``tokens`` (int32, -1 for none) under the rows of ``logits``, with log-sum-exp, entropy
+    and the top alternatives; every output may be None.  The width of the top outputs says how many."""
+    import torch
+    _require(logits.dim() == 2)
+    rows, vocab = logits.shape
+    _vector(tokens, rows, torch.int32)
+    for t in (logprob, lse, entropy):
+        _vector(t, rows, torch.float32)
+    _require((top_logprobs is None) == (top_ids is None))
+    k = 0
+    if top_ids is not None:
+        _require(top_ids.dim() == 2 and top_ids.shape == top_logprobs.shape and top_ids.shape[0] == rows and
+                 top_ids.dtype == torch.int32 and top_logprobs.dtype == torch.float32 and
+                 top_ids.is_contiguous() and top_logprobs.is_contiguous())
+        k = top_ids.shape[1]
+    _on(ctx, logits, tokens, logprob, lse, entropy, top_logprobs, top_ids)
+    _check(lib().peagle_token_logprobs_fwd(ctx.h, _dtype(logits), int(rows), int(vocab), _ptr(logits),
+                                           _ld(logits, rows, vocab), _ptr(tokens), ctypes.c_float(scale), _ptr(logprob),
+                                           _ptr(lse), _ptr(entropy), int(k), _ptr(top_logprobs), _ptr(top_ids),
+                                           _stream_on(ctx, stream)), ctx.h)
+
+
+def peagle_token_logprobs_bwd(ctx, logits, tokens, scale, lse, entropy, g_logprob, g_entropy, dlogits, stream=None):
+    """Gradient of the logits from those of logprob and entropy (either may be None); ``dlogits`` may be ``logits``."""
+    import torch
+    _require(logits.dim() == 2)
+    rows, vocab = logits.shape
+    _require(dlogits.dtype == logits.dtype)
+    _vector(tokens, rows, torch.int32)
+    for t in (lse, entropy, g_logprob, g_entropy):
+        _vector(t, rows, torch.float32)
+    _on(ctx, logits, tokens, lse, entropy, g_logprob, g_entropy, dlogits)
+    _check(lib().peagle_token_logprobs_bwd(ctx.h, _dtype(logits), int(rows), int(vocab), _ptr(logits),
+                                           _ld(logits, rows, vocab), _ptr(tokens), ctypes.c_float(scale), _ptr(lse),
+                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(dlogits),
+                                           _ld(dlogits, rows, vocab), _stream_on(ctx, stream)), ctx.h)
 
 
 def peagle_selftest_wait_expiry(ctx, limit_ms: int = 20, stream=None):

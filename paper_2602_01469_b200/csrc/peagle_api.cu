@@ -1352,6 +1352,98 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
     return PEAGLE_OK;
 }
 
+// ---- token log probabilities
+
+static int logprob_args_ok(int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, float scale)
+{
+    if (!dtype_size(dtype) || rows < 0 || vocab < 1 || ld < vocab || !(scale > 0.f && scale <= 1e20f))
+        return PEAGLE_ERR_BAD_SHAPE;
+    return PEAGLE_OK;
+}
+
+int peagle_token_logprobs_fwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
+                              const void *logits, int64_t ld, const int32_t *tokens, float scale,
+                              float *logprob, float *lse, float *entropy, int32_t top_k,
+                              float *top_logprobs, int32_t *top_ids, void *stream)
+{
+    if (!ctx)
+        return PEAGLE_ERR_NULL;
+    const int rc = logprob_args_ok(dtype, rows, vocab, ld, scale);
+    if (rc != PEAGLE_OK)
+        return rc;
+    if (top_k < 0 || top_k > vocab)
+        return PEAGLE_ERR_BAD_SHAPE;
+    if (top_k > PEAGLE_MAX_TOP_K)
+        return PEAGLE_ERR_TOO_LARGE;
+    if (rows == 0)
+        return PEAGLE_OK;
+    if (!logits || (logprob && !tokens) || (top_k > 0 && (!top_logprobs || !top_ids)))
+        return PEAGLE_ERR_NULL;
+    if (!aligned_to(logits, dtype_size(dtype)) || !aligned_to(tokens, 4) || !aligned_to(logprob, 4) || !aligned_to(lse, 4) ||
+        !aligned_to(entropy, 4) || !aligned_to(top_logprobs, 4) || !aligned_to(top_ids, 4))
+        return PEAGLE_ERR_ALIGN;
+    LogprobArgs a = {};
+    a.dtype = dtype;
+    a.rows = rows;
+    a.vocab = vocab;
+    a.logits = logits;
+    a.ld = ld;
+    a.tokens = tokens;
+    a.scale = scale;
+    a.logprob = logprob;
+    a.lse = lse;
+    a.entropy = entropy;
+    a.top_k = top_k;
+    a.top = top_logprobs;
+    a.ids = top_ids;
+    a.status = ctx->status;
+    const OnDevice on(ctx->device);
+    CK(on.error);
+    ctx->launches += launch_logprobs_fwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    CK(cudaGetLastError());
+    return PEAGLE_OK;
+}
+
+int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
+                              const void *logits, int64_t ld, const int32_t *tokens, float scale,
+                              const float *lse, const float *entropy, const float *g_logprob,
+                              const float *g_entropy, void *dlogits, int64_t ldd, void *stream)
+{
+    if (!ctx)
+        return PEAGLE_ERR_NULL;
+    const int rc = logprob_args_ok(dtype, rows, vocab, ld, scale);
+    if (rc != PEAGLE_OK)
+        return rc;
+    if (ldd < vocab)
+        return PEAGLE_ERR_BAD_SHAPE;
+    if (rows == 0)
+        return PEAGLE_OK;
+    if (!logits || !dlogits || !lse || (g_logprob && !tokens) || (g_entropy && !entropy))
+        return PEAGLE_ERR_NULL;
+    if (!aligned_to(logits, dtype_size(dtype)) || !aligned_to(dlogits, dtype_size(dtype)) || !aligned_to(tokens, 4) ||
+        !aligned_to(lse, 4) || !aligned_to(entropy, 4) || !aligned_to(g_logprob, 4) || !aligned_to(g_entropy, 4))
+        return PEAGLE_ERR_ALIGN;
+    LogprobArgs a = {};
+    a.dtype = dtype;
+    a.rows = rows;
+    a.vocab = vocab;
+    a.logits = logits;
+    a.ld = ld;
+    a.tokens = tokens;
+    a.scale = scale;
+    a.lse_in = lse;
+    a.entropy_in = entropy;
+    a.g_lp = g_logprob;
+    a.g_h = g_entropy;
+    a.dlogits = dlogits;
+    a.ldd = ldd;
+    const OnDevice on(ctx->device);
+    CK(on.error);
+    ctx->launches += launch_logprobs_bwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    CK(cudaGetLastError());
+    return PEAGLE_OK;
+}
+
 int peagle_assign_segments(const int32_t *anchor, const int32_t *depth, int32_t count, int32_t K,
                            const int32_t *boundaries, int32_t S, int32_t *segment_out)
 {

@@ -224,6 +224,25 @@ int launch_norm_fwd(const NormArgs &a, int n_sm, cudaStream_t s);
 size_t norm_bwd_scratch(const NormArgs &a, int n_sm);
 int launch_norm_bwd(const NormArgs &a, int n_sm, cudaStream_t s);
 
+// Token log probabilities (peagle_logprobs.cu).  Row strides in elements.
+struct LogprobArgs {
+    int dtype, rows, vocab;
+    const void *logits;
+    int64_t ld;
+    const int32_t *tokens;
+    float scale;
+    float *logprob, *lse, *entropy; // forward; may be null
+    int top_k;
+    float *top;
+    int32_t *ids;
+    const float *lse_in, *entropy_in, *g_lp, *g_h; // backward; g_lp, g_h may be null
+    void *dlogits;
+    int64_t ldd;
+    int *status;
+};
+int launch_logprobs_fwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
+int launch_logprobs_bwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
+
 // Packed-metadata form of the attention predicate: m = anchor << 8 | depth.
 // (depth_k == 0 and anchor_k <= anchor_q) or (anchor_k == anchor_q and depth_k <= depth_q)
 __host__ __device__ inline bool allowed_packed(int32_t mq, int32_t mk)

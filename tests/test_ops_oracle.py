@@ -61,6 +61,53 @@ def test_norm_closed_forms():
     assert np.allclose(rstd, [1 / np.sqrt(12.5)]) and np.allclose(y, np.array([[3.0, 4.0]]) / np.sqrt(12.5))
 
 
+def test_token_logprobs_equal_torch_and_its_autograd():
+    gen = torch.Generator().manual_seed(4)
+    x = torch.randn(6, 19, generator=gen, dtype=torch.float64, requires_grad=True)
+    tokens = torch.tensor([3, 0, 18, 7, -1, 2])
+    g, h = torch.randn(6, generator=gen, dtype=torch.float64), torch.randn(6, generator=gen, dtype=torch.float64)
+    logp = torch.log_softmax(x * 0.7, 1)
+    lp = torch.where(tokens < 0, 0.0, logp.gather(1, tokens.clamp(min=0)[:, None])[:, 0])
+    H = torch.distributions.Categorical(logits=x * 0.7).entropy()
+    (lp * g + H * h).sum().backward()
+    got = oo.token_logprobs(x.detach().numpy(), tokens.numpy(), 0.7, 4)
+    assert np.allclose(got[0], lp.detach().numpy(), atol=1e-13) and np.allclose(got[2], H.detach().numpy(), atol=1e-13)
+    assert np.allclose(got[1], torch.logsumexp(x * 0.7, 1).detach().numpy(), atol=1e-13)
+    best = torch.topk(logp, 4, 1)
+    assert np.allclose(got[3], best.values.detach().numpy(), atol=1e-13) and np.array_equal(got[4], best.indices.numpy())
+    d = oo.token_logprobs_bwd(x.detach().numpy(), tokens.numpy(), 0.7, got[1], got[2], g.numpy(), h.numpy())
+    assert np.allclose(d, x.grad.numpy(), atol=1e-13)
+
+
+def test_token_logprobs_by_central_differences():
+    rng = np.random.default_rng(2)
+    x, tokens = rng.standard_normal((2, 9)), np.array([4, 8])
+    g, h = rng.standard_normal(2), rng.standard_normal(2)
+
+    def loss(x):
+        lp, _, H, _, _ = oo.token_logprobs(x, tokens, 1.3, 0)
+        return float((lp * g + H * h).sum())
+
+    _, lse, H, _, _ = oo.token_logprobs(x, tokens, 1.3, 0)
+    d = oo.token_logprobs_bwd(x, tokens, 1.3, lse, H, g, h)
+    for i in np.ndindex(2, 9):
+        up, dn = x.copy(), x.copy()
+        up[i] += 1e-5
+        dn[i] -= 1e-5
+        assert (loss(up) - loss(dn)) / 2e-5 == pytest.approx(d[i], rel=1e-6, abs=1e-8)
+
+
+def test_token_logprobs_of_rows_without_a_distribution():
+    inf, nan = np.inf, np.nan
+    x = np.array([[-inf, -inf, -inf], [0.0, nan, 1.0], [inf, 0.0, 0.0], [-inf, 2.0, -inf], [5.0, 5.0, 5.0], [0.0, -0.0, 1.0]])
+    lp, lse, H, top, ids = oo.token_logprobs(x, np.array([1, 0, 2, 1, 2, 7]), 1.0, 2)
+    assert lp[0] == lse[0] == -inf and H[0] == 0 and ids[0].tolist() == [0, 1] and np.isneginf(top[0]).all()
+    assert np.isnan([lp[1], lse[1], H[1], lp[2], lse[2], H[2]]).all() and (ids[1:3] == -1).all()
+    assert lp[3] == 0 and lse[3] == 2 and H[3] == 0 and ids[3].tolist() == [1, 0]
+    assert lp[4] == pytest.approx(-np.log(3)) and H[4] == pytest.approx(np.log(3)) and ids[4].tolist() == [0, 1]
+    assert np.isnan(lp[5]) and ids[5].tolist() == [2, 0]
+
+
 # ------------------------------------------------------------------ refusals, before any device is touched
 @pytest.fixture(scope="module")
 def lib():
@@ -113,3 +160,46 @@ def test_norm_refusals_of_one_direction(lib, zeros):
     assert _norm_call(lib, zeros, True, dY=0) == S["NULL"]
     assert _norm_call(lib, zeros, True, lddy=10) == S["BAD_SHAPE"]
     assert _norm_call(lib, None, False) == _norm_call(lib, None, True) == S["NULL"]
+
+
+def _logprob_call(lib, ctx, back, **over):
+    import ctypes
+    a = dict(dtype=1, rows=4, vocab=100, logits=4096, ld=100, tokens=8192, scale=1.0, lp=12288, lse=16384, H=0, k=0, top=0,
+             ids=0, g=20480, h=0, d=24576, ldd=100)
+    a.update(over)
+    i32, i64, ptr = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
+    head = [ctx, i32(a["dtype"]), i32(a["rows"]), i32(a["vocab"]), ptr(a["logits"]), i64(a["ld"]), ptr(a["tokens"]),
+            ctypes.c_float(a["scale"])]
+    if back:
+        return lib.peagle_token_logprobs_bwd(*head, ptr(a["lse"]), ptr(a["H"]), ptr(a["g"]), ptr(a["h"]), ptr(a["d"]),
+                                             i64(a["ldd"]), ptr(0))
+    return lib.peagle_token_logprobs_fwd(*head, ptr(a["lp"]), ptr(a["lse"]), ptr(a["H"]), i32(a["k"]), ptr(a["top"]),
+                                         ptr(a["ids"]), ptr(0))
+
+
+@pytest.mark.parametrize("back", [False, True])
+@pytest.mark.parametrize("over,status", [
+    ({"rows": 0}, "OK"), ({"rows": -2}, "BAD_SHAPE"), ({"vocab": 0}, "BAD_SHAPE"), ({"ld": 99}, "BAD_SHAPE"),
+    ({"dtype": 5}, "BAD_SHAPE"), ({"scale": 0.0}, "BAD_SHAPE"), ({"scale": -1.0}, "BAD_SHAPE"),
+    ({"scale": float("nan")}, "BAD_SHAPE"), ({"scale": float("inf")}, "BAD_SHAPE"), ({"logits": 0}, "NULL"),
+    ({"tokens": 0}, "NULL"), ({"logits": 4097}, "ALIGN"), ({"tokens": 8194}, "ALIGN"), ({"lse": 16386}, "ALIGN"),
+])
+def test_logprob_refusals(lib, zeros, back, over, status):
+    from paper_2602_01469_b200 import binding
+    assert _logprob_call(lib, zeros, back, **over) == binding.STATUS[status]
+
+
+def test_logprob_refusals_of_one_direction(lib, zeros):
+    from paper_2602_01469_b200 import binding
+    S = binding.STATUS
+    assert _logprob_call(lib, zeros, False, k=-1) == S["BAD_SHAPE"]
+    assert _logprob_call(lib, zeros, False, k=101, top=4096, ids=4096) == S["BAD_SHAPE"]
+    assert _logprob_call(lib, zeros, False, k=65, top=4096, ids=4096) == S["TOO_LARGE"]
+    assert _logprob_call(lib, zeros, False, k=3, top=4096) == S["NULL"]
+    assert _logprob_call(lib, zeros, False, k=3, ids=4096) == S["NULL"]
+    assert _logprob_call(lib, zeros, True, lse=0) == S["NULL"]
+    assert _logprob_call(lib, zeros, True, d=0) == S["NULL"]
+    assert _logprob_call(lib, zeros, True, h=4096) == S["NULL"]          # the entropy's gradient without the entropy
+    assert _logprob_call(lib, zeros, True, ldd=99) == S["BAD_SHAPE"]
+    assert _logprob_call(lib, zeros, True, d=24577) == S["ALIGN"]
+    assert _logprob_call(lib, None, False) == _logprob_call(lib, None, True) == S["NULL"]
