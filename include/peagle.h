@@ -382,6 +382,51 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
                               const float *g_entropy, void *dlogits, int64_t ldd, void *stream);
 
 /*
+ * One AdamW step over many tensors, in place (Section 5.1 trains the drafter; the optimizer takes the gradients
+ * that the calls above sum up).  With g = grad * grad_scale and t the step's number, 1 for the first:
+ *     m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2
+ *     param -= lr weight_decay param + lr (m / (1 - beta1^t)) / (sqrt(v / (1 - beta2^t)) + eps)
+ * A tensor is `count` contiguous elements of param_dtype with gradients of grad_dtype.  With `master` (dev fp32,
+ * bf16 parameters only) the step is taken on the masters and param is their rounding; without it param itself is
+ * read, stepped in fp32 and rounded.
+ *   States in 32 bits: m, v dev fp32, m_scale = v_scale = NULL.
+ *   States in 8 bits: m, v dev e4m3 codes (1 byte each) with dev fp32 scales, one per PEAGLE_ADAMW_BLOCK elements
+ * (the last block may be short): m = code * m_scale and sqrt(v) = code * v_scale.  A scale is the power of two that
+ * brings the block's largest magnitude into [128, 256), at least 2^-107.  Rounding to the codes is stochastic, up with
+ * the probability of the fraction, because to the nearest an average with beta2 near 1 would never move: its steps
+ * are smaller than half a code.  (A root above zero is never stored as zero, it divides the next step.)  The random
+ * bits are a hash of (seed, step, place of the tensor in the list, element), so a step repeats bit for bit; the new
+ * m and v are formed in fp64 and rounded to fp32 before that.  An element whose new state is not finite is stored as
+ * NaN and does not count for its block's scale.  All zero codes and any scales are the states to begin with.
+ * lr_dev, step_dev, grad_scale_dev (dev, each may be NULL) replace lr, step and the factor 1, so that a captured
+ * graph can be replayed with others.  lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0, step >= 1 (not checked on
+ * the device).  Tensors must not share memory.  `tensors` is a host array, read before the call returns; a launch
+ * takes PEAGLE_ADAMW_TENSORS of them.  Asynchronous; nothing is allocated.
+ */
+#define PEAGLE_ADAMW_BLOCK 256
+#define PEAGLE_ADAMW_TENSORS 384
+typedef struct peagle_adamw_tensor {
+    void *param;
+    const void *grad;
+    float *master;           /* NULL: none */
+    void *m, *v;
+    float *m_scale, *v_scale; /* both NULL: states in 32 bits */
+    int64_t count;
+    int32_t param_dtype, grad_dtype;
+    float weight_decay;
+} peagle_adamw_tensor_t;
+typedef struct peagle_adamw {
+    double lr, beta1, beta2, eps;
+    int64_t step;
+    const float *lr_dev;
+    const int64_t *step_dev;
+    const float *grad_scale_dev;
+    uint32_t seed;
+} peagle_adamw_t;
+int peagle_adamw_step(peagle_ctx *ctx, const peagle_adamw_t *how, const peagle_adamw_tensor_t *tensors,
+                      int32_t n_tensors, void *stream);
+
+/*
  * Algorithm 1, host only: segment of every token.  `boundaries` is host [S+1], context-token
  * positions with boundaries[0]=0 and boundaries[S]=n (Algorithm 1's B).  Depth 0 and 1 tokens
  * go by their position anchor+depth (a position at or beyond n stays in the last segment);

@@ -29,6 +29,7 @@ EXPORTS = [
     "peagle_rope_qkv_fwd", "peagle_rope_qkv_bwd", "peagle_attn_partitioned_acc", "peagle_cast_grads",
     "peagle_gemm_bf16", "peagle_layer_partitioned", "peagle_selftest_wait_expiry",
     "peagle_norm_fwd", "peagle_norm_bwd", "peagle_token_logprobs_fwd", "peagle_token_logprobs_bwd",
+    "peagle_adamw_step",
 ]
 
 NORM = {"layer": 0, "rms": 1}  # peagle_norm
@@ -59,6 +60,23 @@ class peagle_partition_t(ctypes.Structure):
         ("q", peagle_range_t),
         ("k", ctypes.POINTER(peagle_range_t)),
         ("nk", ctypes.c_int32),
+    ]
+
+
+class peagle_adamw_tensor_t(ctypes.Structure):
+    _fields_ = [
+        ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("master", ctypes.c_void_p),
+        ("m", ctypes.c_void_p), ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("count", ctypes.c_int64), ("param_dtype", ctypes.c_int32), ("grad_dtype", ctypes.c_int32),
+        ("weight_decay", ctypes.c_float),
+    ]
+
+
+class peagle_adamw_t(ctypes.Structure):
+    _fields_ = [
+        ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+        ("step", ctypes.c_int64), ("lr_dev", ctypes.c_void_p), ("step_dev", ctypes.c_void_p),
+        ("grad_scale_dev", ctypes.c_void_p), ("seed", ctypes.c_uint32),
     ]
 
 
@@ -189,6 +207,59 @@ def _partition_array(parts):
     for i, p in enumerate(parts):
         arr[i] = p.c
     return arr
+
+
+ADAMW_BLOCK = 256  # elements that share a scale where states are held in 8 bits
+
+
+class AdamWTensors:
+    """The tensors of ``peagle_adamw_step``, put together once: owns the array a call passes and keeps the tensors
+    alive.  Each item is a dict of ``param``, ``grad``, ``m``, ``v`` and, where they apply, ``master`` (fp32, for bf16
+    parameters), ``m_scale`` and ``v_scale`` (states in 8 bits: m and v are float8_e4m3fn, a scale for every
+    ADAMW_BLOCK elements), ``weight_decay``.  Contiguous device tensors; no two may share memory."""
+
+    def __init__(self, items):
+        import torch
+        self.items = [dict(i) for i in items]
+        self.device = self.items[0]["param"].device.index if self.items else None
+        self.c = (peagle_adamw_tensor_t * max(len(self.items), 1))()
+        written = []
+        for c, i in zip(self.c, self.items):
+            p, n = i["param"], i["param"].numel()
+            eight = i.get("m_scale") is not None
+            state = torch.float8_e4m3fn if eight else torch.float32
+            for name, dtype, count in (("master", torch.float32, n), ("m", state, n), ("v", state, n),
+                                       ("m_scale", torch.float32, -(-n // ADAMW_BLOCK)),
+                                       ("v_scale", torch.float32, -(-n // ADAMW_BLOCK))):
+                t = i.get(name)
+                if t is None:
+                    _require(name == "master" or (name.endswith("scale") and not eight))
+                    continue
+                _require(t.dtype == dtype and t.numel() == count and t.is_contiguous())
+                self._own(t)
+                written.append((t.data_ptr(), t.numel() * t.element_size()))
+                setattr(c, name, t.data_ptr())
+            _require(p.is_contiguous())
+            self._own(p)
+            written.append((p.data_ptr(), n * p.element_size()))
+            c.param, c.count, c.param_dtype = p.data_ptr(), n, _dtype(p)
+            c.weight_decay = float(i.get("weight_decay", 0.0))
+        written = sorted(w for w in written if w[1])
+        _require(all(a + size <= b for (a, size), (b, _) in zip(written, written[1:])), "BAD_RANGE")
+        self.set_grads([i["grad"] for i in self.items])
+
+    def _own(self, t):
+        _require(t.is_cuda and t.device.index == self.device)
+
+    def set_grads(self, grads):
+        """Other gradients for the steps to come, in the order of the tensors."""
+        grads = list(grads)
+        _require(len(grads) == len(self.items))
+        for c, i, g in zip(self.c, self.items, grads):
+            _require(g.numel() == c.count and g.is_contiguous())
+            self._own(g)
+            c.grad, c.grad_dtype = g.data_ptr(), _dtype(g)
+            i["grad"] = g
 
 
 class Context:
@@ -391,6 +462,20 @@ def peagle_token_logprobs_bwd(ctx, logits, tokens, scale, lse, entropy, g_logpro
                                            _ld(logits, rows, vocab), _ptr(tokens), ctypes.c_float(scale), _ptr(lse),
                                            _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(dlogits),
                                            _ld(dlogits, rows, vocab), _stream_on(ctx, stream)), ctx.h)
+
+
+def peagle_adamw_step(ctx, tensors: AdamWTensors, lr, beta1, beta2, eps, step=1, seed=0, lr_dev=None, step_dev=None,
+                      grad_scale=None, stream=None):
+    """One AdamW step over ``tensors``, in place.  ``lr_dev`` (fp32), ``step_dev`` (int64) and ``grad_scale`` (fp32) are
+    one-element device tensors that replace lr, step and the gradients' factor 1."""
+    import torch
+    for t, dtype in ((lr_dev, torch.float32), (step_dev, torch.int64), (grad_scale, torch.float32)):
+        _require(t is None or (t.numel() == 1 and t.dtype == dtype))
+    _on(ctx, lr_dev, step_dev, grad_scale)
+    _require(tensors.device is None or tensors.device == ctx.device)
+    how = peagle_adamw_t(float(lr), float(beta1), float(beta2), float(eps), int(step), _ptr(lr_dev), _ptr(step_dev),
+                         _ptr(grad_scale), int(seed) & 0xFFFFFFFF)
+    _check(lib().peagle_adamw_step(ctx.h, ctypes.byref(how), tensors.c, len(tensors.items), _stream_on(ctx, stream)), ctx.h)
 
 
 def peagle_selftest_wait_expiry(ctx, limit_ms: int = 20, stream=None):

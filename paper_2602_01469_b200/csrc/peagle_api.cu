@@ -1444,6 +1444,45 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
     return PEAGLE_OK;
 }
 
+// ---- optimizer
+
+int peagle_adamw_step(peagle_ctx *ctx, const peagle_adamw_t *how, const peagle_adamw_tensor_t *tensors,
+                      int32_t n_tensors, void *stream)
+{
+    if (!ctx || !how || (n_tensors > 0 && !tensors))
+        return PEAGLE_ERR_NULL;
+    const double huge = 1e30;
+    if (n_tensors < 0 || !(how->lr >= 0.0 && how->lr <= huge) || !(how->beta1 >= 0.0 && how->beta1 < 1.0) ||
+        !(how->beta2 >= 0.0 && how->beta2 < 1.0) || !(how->eps > 0.0 && how->eps <= huge) ||
+        (!how->step_dev && how->step < 1))
+        return PEAGLE_ERR_BAD_SHAPE;
+    if (!aligned_to(how->lr_dev, 4) || !aligned_to(how->step_dev, 8) || !aligned_to(how->grad_scale_dev, 4))
+        return PEAGLE_ERR_ALIGN;
+    int64_t elements = 0;
+    for (int32_t i = 0; i < n_tensors; ++i) {
+        const peagle_adamw_tensor_t &t = tensors[i];
+        const size_t ps = dtype_size(t.param_dtype), gs = dtype_size(t.grad_dtype);
+        if (!ps || !gs || t.count < 0 || !(t.weight_decay >= 0.f && t.weight_decay <= 1e30f) ||
+            (t.master && t.param_dtype != PEAGLE_BF16) || (t.m_scale != nullptr) != (t.v_scale != nullptr))
+            return PEAGLE_ERR_BAD_SHAPE;
+        if (t.count == 0)
+            continue;
+        if (!t.param || !t.grad || !t.m || !t.v)
+            return PEAGLE_ERR_NULL;
+        const size_t ss = t.m_scale ? 1 : 4;
+        if (!aligned_to(t.param, ps) || !aligned_to(t.grad, gs) || !aligned_to(t.master, 4) || !aligned_to(t.m, ss) ||
+            !aligned_to(t.v, ss) || !aligned_to(t.m_scale, 4) || !aligned_to(t.v_scale, 4))
+            return PEAGLE_ERR_ALIGN;
+        if (t.count > (int64_t)1 << 40 || (elements += t.count) > (int64_t)1 << 40)
+            return PEAGLE_ERR_TOO_LARGE;
+    }
+    const OnDevice on(ctx->device);
+    CK(on.error);
+    ctx->launches += launch_adamw(*how, tensors, n_tensors, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    CK(cudaGetLastError());
+    return PEAGLE_OK;
+}
+
 int peagle_assign_segments(const int32_t *anchor, const int32_t *depth, int32_t count, int32_t K,
                            const int32_t *boundaries, int32_t S, int32_t *segment_out)
 {

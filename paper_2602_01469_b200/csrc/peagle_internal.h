@@ -243,6 +243,10 @@ struct LogprobArgs {
 int launch_logprobs_fwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
 int launch_logprobs_bwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
 
+// AdamW over a list of tensors (peagle_adamw.cu).  The arguments have been checked.  Returns the number of
+// kernels launched.
+int launch_adamw(const peagle_adamw_t &how, const peagle_adamw_tensor_t *tensors, int n, int n_sm, cudaStream_t s);
+
 // Packed-metadata form of the attention predicate: m = anchor << 8 | depth.
 // (depth_k == 0 and anchor_k <= anchor_q) or (anchor_k == anchor_q and depth_k <= depth_q)
 __host__ __device__ inline bool allowed_packed(int32_t mq, int32_t mk)

@@ -1,0 +1,262 @@
+"""GPU: the AdamW step over lists of tensors, states in 32 and in 8 bits, through the C ABI, against the fp64
+definition.
+
+Tolerances, U = 2^-24.  m = b1 m + (1 - b1) g: the two factors, the scaled gradient, two products and the sum are
+rounded: 5 U (|b1 m| + |(1 - b1) g|).  v likewise with one product more, all terms positive: 6 U v.  The update
+m / (sqrt(v) c + eps) lr': half of v's error, the root, c, the fused sum, the quotient (two units), lr' and the product:
+16 U of itself, and m's error passed on.  p: its decay and the difference are rounded, 3 U (|p| + |update|), then to its
+type.  States in 8 bits are compared bit for bit, the step that they take like one with the m and root that they
+stand for."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops_oracle as oo
+from paper_2602_01469_b200 import binding
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+U = 2.0 ** -24
+HALF = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}
+BF16, F32 = torch.bfloat16, torch.float32
+F8 = torch.float8_e4m3fn
+HOW = dict(lr=3e-3, beta1=0.9, beta2=0.98, eps=1e-7)
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = binding.Context(0)
+    yield c
+    c.close()
+
+
+def f64(t):
+    return t.detach().double().cpu().numpy()
+
+
+def make(gen, n, dtype, gdtype, bits, master, decay, offset=0):
+    """One tensor of n elements in the middle of longer buffers (``offset`` elements in), with what follows it."""
+    def put(x):
+        buf = torch.full((n + offset + 40,), 1.0, dtype=torch.float32).to(x.dtype).to(DEV)
+        buf[offset:offset + n] = x.to(DEV)
+        return buf[offset:offset + n]
+
+    w = torch.randn(n, generator=gen)
+    # gradients over several decades, a stretch of zeros, exact zeros among the states
+    g = torch.randn(n, generator=gen) * torch.exp(3 * torch.randn(n, generator=gen)) * 1e-3
+    g[n // 3: n // 3 + n // 7] = 0
+    m, root = 0.5 * torch.randn(n, generator=gen) * g.abs(), g.abs() * (0.5 + torch.rand(n, generator=gen))
+    item = {"grad": put(g.to(gdtype)), "weight_decay": decay, "master": put(w) if master else None, "param": put(w.to(dtype))}
+    if bits == 32:
+        item.update(m=put(m), v=put(root ** 2))
+    else:
+        blocks = -(-n // 256)
+        ms = torch.tensor(oo.block_scale(m.double().numpy()), dtype=F32)
+        vs = torch.tensor(oo.block_scale(root.double().numpy()), dtype=F32)
+        per = lambda s: s.repeat_interleave(256)[:n]
+        item.update(m=put((m / per(ms)).to(F8).view(torch.uint8)).view(F8), v=put((root / per(vs)).to(F8).view(torch.uint8)).view(F8),
+                    m_scale=ms.to(DEV), v_scale=vs.to(DEV))
+        assert ms.shape[0] == blocks
+    return item
+
+
+def snapshot(item):
+    return {k: (t.clone() if isinstance(t, torch.Tensor) else t) for k, t in item.items()}
+
+
+def outside(got, want, bound):
+    bad = ~((np.abs(got - want) <= bound) | (np.isnan(got) & np.isnan(want)))
+    assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+def check(before, after, place, step, seed, how=HOW, factor=1.0):
+    n = before["param"].numel()
+    p = f64(before["master"] if before["master"] is not None else before["param"]).ravel()
+    g = f64((before["grad"].float().cpu() * np.float32(factor))).ravel()
+    b1, b2 = how["beta1"], how["beta2"]
+    if "m_scale" in before:
+        code = lambda t: t.view(torch.uint8).cpu().numpy().ravel()
+        m, root, mc, vc, ms, vs = oo.adamw_states8(g, code(before["m"]), code(before["v"]), f64(before["m_scale"]),
+                                                   f64(before["v_scale"]), b1, b2, seed, step, place)
+        assert np.array_equal(f64(after["m_scale"]), ms) and np.array_equal(f64(after["v_scale"]), vs)
+        assert np.array_equal(oo.e4m3_values()[code(after["m"])], oo.e4m3_values()[mc], equal_nan=True)
+        assert np.array_equal(oo.e4m3_values()[code(after["v"])], oo.e4m3_values()[vc], equal_nan=True)
+        m, v, em = m.astype(np.float64), root.astype(np.float64) ** 2, U * np.abs(m.astype(np.float64))
+    else:
+        m0, v0 = f64(before["m"]).ravel(), f64(before["v"]).ravel()
+        _, m, v = oo.adamw(p, g, m0, v0, how["lr"], b1, b2, how["eps"], 0.0, step)
+        em = 5 * U * (np.abs(b1 * m0) + np.abs((1 - b1) * g))
+        outside(f64(after["m"]).ravel(), m, em + 2.0 ** -126)
+        outside(f64(after["v"]).ravel(), v, 6 * U * v + 2.0 ** -126)
+    lr = how["lr"] / (1 - b1 ** step)
+    below = np.sqrt(v / (1 - b2 ** step)) + how["eps"]
+    update = lr * m / below
+    want = p - how["lr"] * float(np.float32(before["weight_decay"])) * p - update
+    err = 16 * U * np.abs(update) + lr * em / below + 3 * U * (np.abs(p) + np.abs(update))
+    if before["master"] is not None:
+        outside(f64(after["master"]).ravel(), want, err)
+        assert torch.equal(after["param"], after["master"].to(BF16))
+    else:
+        dt = after["param"].dtype
+        outside(f64(after["param"]).ravel(), want, HALF[dt] * np.abs(want) + err)
+    assert n == after["param"].numel()
+
+
+KINDS = [  # param, grad, bits, master
+    (F32, F32, 32, False), (BF16, BF16, 32, True), (BF16, F32, 32, True), (BF16, BF16, 32, False), (F32, BF16, 32, False),
+    (F32, F32, 8, False), (BF16, BF16, 8, True), (BF16, BF16, 8, False), (BF16, F32, 8, True),
+]
+SIZES = [1, 7, 255, 256, 257, 1000, 2048, 4096 + 8, 20011]
+
+
+@pytest.mark.parametrize("dtype,gdtype,bits,master", KINDS)
+def test_lists_of_tensors(ctx, dtype, gdtype, bits, master):
+    gen = torch.Generator().manual_seed(bits + int(master))
+    items = [make(gen, n, dtype, gdtype, bits, master, 0.1 * (i % 3), offset=i % 4) for i, n in enumerate(SIZES)]
+    items.insert(3, make(gen, 0, dtype, gdtype, bits, master, 0.0))
+    items.append(make(gen, 0, dtype, gdtype, bits, master, 0.0))
+    tensors = binding.AdamWTensors(items)
+    for step in (1, 2, 50):
+        before = [snapshot(i) for i in items]
+        behind = [i["param"]._base[-30:].clone() if i["param"]._base is not None else None for i in items]
+        binding.peagle_adamw_step(ctx, tensors, step=step, seed=77, **HOW)
+        torch.cuda.synchronize()
+        for k, (b, a) in enumerate(zip(before, items)):
+            check(b, a, k, step, 77)
+            if behind[k] is not None:
+                assert torch.equal(a["param"]._base[-30:], behind[k])
+    assert binding.peagle_poll_status(ctx) == 0
+
+
+def test_mixed_kinds_and_more_tensors_than_a_launch_takes(ctx):
+    gen = torch.Generator().manual_seed(5)
+    items = [make(gen, 1 + (i * 37) % 600, *KINDS[i % len(KINDS)], 0.01, offset=i % 3) for i in range(900)]
+    before = [snapshot(i) for i in items]
+    n = binding.peagle_launch_count(ctx)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors(items), step=3, seed=1, **HOW)
+    torch.cuda.synchronize()
+    assert binding.peagle_launch_count(ctx) - n == 3             # 384 tensors each
+    for k, (b, a) in enumerate(zip(before, items)):
+        check(b, a, k, 3, 1)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_large_tensor(ctx, bits):
+    gen = torch.Generator().manual_seed(6)
+    item = make(gen, 3_000_001, BF16, BF16, bits, True, 0.1)
+    before = snapshot(item)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors([item]), step=4, seed=9, **HOW)
+    torch.cuda.synchronize()
+    check(before, item, 0, 4, 9)
+
+
+def test_states_that_begin_at_zero(ctx):
+    gen = torch.Generator().manual_seed(7)
+    item = make(gen, 700, F32, F32, 8, False, 0.0)
+    for name in ("m", "v"):
+        item[name].view(torch.uint8).zero_()
+        item[name + "_scale"].zero_()
+    before = snapshot(item)
+    tensors = binding.AdamWTensors([item])
+    binding.peagle_adamw_step(ctx, tensors, step=1, seed=2, **HOW)
+    torch.cuda.synchronize()
+    check(before, item, 0, 1, 2)
+    item["grad"].zero_()
+    for step in range(2, 5):
+        before = snapshot(item)
+        binding.peagle_adamw_step(ctx, tensors, step=step, seed=2, **HOW)
+        check(before, item, 0, step, 2)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_bad_gradient_stays_in_its_element(ctx, bits):
+    gen = torch.Generator().manual_seed(8)
+    item = make(gen, 600, F32, F32, bits, False, 0.1)
+    clean = snapshot(item)
+    tensors = binding.AdamWTensors([item])
+    for at, bad in ((10, float("nan")), (300, float("inf")), (301, -float("inf"))):
+        item["grad"][at] = bad
+        clean["grad"][at] = 0
+    binding.peagle_adamw_step(ctx, tensors, step=2, seed=3, **HOW)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors([clean]), step=2, seed=3, **HOW)
+    torch.cuda.synchronize()
+    keep = torch.ones(600, dtype=torch.bool, device=DEV)
+    keep[[10, 300, 301]] = False
+    assert torch.equal(item["param"][keep], clean["param"][keep])
+    assert torch.isnan(item["param"][~keep]).all()
+    if bits == 8:
+        assert torch.isnan(item["m"].float()[~keep]).all() and torch.isnan(item["v"].float()[~keep]).all()
+        assert torch.equal(item["m"].view(torch.uint8)[keep], clean["m"].view(torch.uint8)[keep])
+        assert torch.equal(item["v_scale"], clean["v_scale"])
+
+
+def test_steps_in_a_captured_graph(ctx):
+    """The step's number, the rate and the gradients' factor on the device: replays equal eager steps bit for bit."""
+    gen = torch.Generator().manual_seed(9)
+    items = [make(gen, 5000, BF16, BF16, b, True, 0.1) for b in (8, 32)]
+    other = [snapshot(i) for i in items]
+    tensors, eager = binding.AdamWTensors(items), binding.AdamWTensors(other)
+    step = torch.zeros(1, dtype=torch.int64, device=DEV)
+    lr, factor = torch.tensor([1e-3], device=DEV), torch.tensor([0.5], device=DEV)
+    betas = dict(beta1=0.9, beta2=0.98, eps=1e-7)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step.add_(1)
+        binding.peagle_adamw_step(ctx, tensors, 0.0, step=0, seed=4, lr_dev=lr, step_dev=step, grad_scale=factor, **betas)
+    for k in range(1, 5):
+        rate = 1e-3 * k
+        lr.fill_(rate)
+        before = snapshot(other[1])
+        g.replay()
+        binding.peagle_adamw_step(ctx, eager, float(np.float32(rate)), step=k, seed=4, grad_scale=factor, **betas)
+        torch.cuda.synchronize()
+        check(before, other[1], 1, k, 4, dict(lr=float(np.float32(rate)), **betas), 0.5)
+        for a, b in zip(items, other):
+            for name in ("param", "master", "m", "v"):
+                assert torch.equal(a[name].view(torch.uint8), b[name].view(torch.uint8)), name
+
+
+def test_an_average_held_in_8_bits_moves(ctx):
+    """beta2 = 0.999 moves v by a thousandth a step, a code is 6 to 12 % away: the average still finds the mean
+    square of the gradients, from above.  (The root is rounded without bias, so its square is a few per cent high.)"""
+    n = 1 << 14
+    gen = torch.Generator(device=DEV).manual_seed(10)
+    item = {"param": torch.zeros(n, device=DEV), "grad": torch.zeros(n, device=DEV), "m": torch.zeros(n, device=DEV).to(F8),
+            "v": torch.full((n,), 128.0, device=DEV).to(F8), "m_scale": torch.ones(n // 256, device=DEV),
+            "v_scale": torch.full((n // 256,), 4.0 / 128, device=DEV)}
+    tensors = binding.AdamWTensors([item])
+    for step in range(1, 4001):
+        item["grad"].normal_(generator=gen)
+        binding.peagle_adamw_step(ctx, tensors, 0.0, 0.9, 0.999, 1e-8, step=step, seed=step)
+    root = item["v"].float().view(-1, 256) * item["v_scale"][:, None]
+    # from 16 towards 1: 16 * 0.999^4000 = 0.29 is left of the start
+    assert 1.0 < float(root.square().mean()) < 1.6
+
+
+def test_set_grads_and_refusals(ctx):
+    gen = torch.Generator().manual_seed(11)
+    item = make(gen, 300, BF16, BF16, 32, False, 0.0)
+    tensors = binding.AdamWTensors([item])
+    fresh = torch.randn(300, generator=gen).to(DEV)
+    tensors.set_grads([fresh])
+    before = snapshot(tensors.items[0])
+    binding.peagle_adamw_step(ctx, tensors, step=1, **HOW)
+    torch.cuda.synchronize()
+    check(before, item, 0, 1, 0)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors([]), step=1, **HOW)     # nothing to do
+
+    def refused(status, f, *args, **kw):
+        with pytest.raises(binding.PeagleError) as e:
+            f(*args, **kw)
+        assert e.value.status == binding.STATUS[status]
+
+    for change in ({"m": item["m"].half()}, {"m": item["m"][:200]}, {"param": item["param"].half()}, {"v": None},
+                   {"master": item["m"].to(BF16)}, {"m_scale": torch.ones(2, device=DEV)}, {"grad": item["grad"][:10]},
+                   {"grad": item["grad"].cpu()}, {"m": item["m"].cpu()}):
+        refused("BAD_SHAPE", binding.AdamWTensors, [{**item, **change}])
+    refused("BAD_RANGE", binding.AdamWTensors, [item, item])                    # the same tensor twice
+    refused("BAD_RANGE", binding.AdamWTensors, [{**item, "v": item["m"]}])
+    refused("BAD_SHAPE", tensors.set_grads, [])
+    refused("BAD_SHAPE", binding.peagle_adamw_step, ctx, tensors, 1e-3, 0.9, 0.99, 1e-8, step=0)
+    refused("BAD_SHAPE", binding.peagle_adamw_step, ctx, tensors, 1e-3, 0.9, 0.99, 1e-8, step_dev=torch.ones(1, device=DEV))

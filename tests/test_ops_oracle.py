@@ -108,6 +108,52 @@ def test_token_logprobs_of_rows_without_a_distribution():
     assert np.isnan(lp[5]) and ids[5].tolist() == [2, 0]
 
 
+def test_adamw_equals_torch():
+    rng = np.random.default_rng(3)
+    p0 = rng.standard_normal(20)
+    p = torch.tensor(p0, requires_grad=True)
+    opt = torch.optim.AdamW([p], lr=0.01, betas=(0.8, 0.95), eps=1e-6, weight_decay=0.3)
+    q, m, v = p0, np.zeros(20), np.zeros(20)
+    for step in range(1, 6):
+        g = rng.standard_normal(20)
+        p.grad = torch.tensor(g)
+        opt.step()
+        q, m, v = oo.adamw(q, g, m, v, 0.01, 0.8, 0.95, 1e-6, 0.3, step)
+    assert np.allclose(q, p.detach().numpy(), atol=1e-14)
+
+
+def test_e4m3_values_equal_torch():
+    codes = torch.arange(256, dtype=torch.uint8)
+    assert np.array_equal(oo.e4m3_values(), codes.view(torch.float8_e4m3fn).double().numpy(), equal_nan=True)
+
+
+def test_stochastic_code_is_unbiased_and_neighbouring():
+    """Over all 2^16 values of the random bits, the mean is the number itself to 2^-16 of a step."""
+    values = oo.e4m3_values()
+    bits = np.arange(1 << 16, dtype=np.float64)
+    for y in (0.0, 0.3 * 2.0 ** -9, 2.0 ** -9, 0.0137, 0.015625, 0.017, 1.03, 100.7, 255.9, 256.0, -3.3):
+        got = values[oo.stochastic_code(np.full(1 << 16, y), bits, False)]
+        step = 2.0 ** -9 if abs(y) < 2.0 ** -6 else 2.0 ** (np.floor(np.log2(abs(y))) - 3)
+        assert abs(got.mean() - y) <= step * 2.0 ** -15 and np.abs(got - y).max() < step
+        if y > 0:
+            assert values[oo.stochastic_code(np.full(1 << 16, y), bits, True)].min() > 0
+
+
+def test_block_scales():
+    x = np.zeros(700)
+    x[3], x[300], x[301] = -5.0, 2.0 ** -120, np.inf
+    assert oo.block_scale(x).tolist() == [2.0 ** -5, 2.0 ** -107, 2.0 ** -107]
+    assert oo.block_scale(np.array([1.0, np.nan])).tolist() == [2.0 ** -7]
+
+
+def test_random_bits_are_spread():
+    b = oo.adamw_random_bits(1, 2, 3, 1 << 16)
+    for part in (b & np.uint64(0xFFFF), b >> np.uint64(16)):
+        counts = np.bincount((part >> np.uint64(12)).astype(int), minlength=16)
+        assert np.abs(counts - 4096).max() < 6 * 64          # six standard deviations
+    assert len(np.unique(np.concatenate([b, oo.adamw_random_bits(1, 2, 4, 1 << 16)]))) > 2 * (1 << 16) - 20
+
+
 # ------------------------------------------------------------------ refusals, before any device is touched
 @pytest.fixture(scope="module")
 def lib():
@@ -203,3 +249,41 @@ def test_logprob_refusals_of_one_direction(lib, zeros):
     assert _logprob_call(lib, zeros, True, ldd=99) == S["BAD_SHAPE"]
     assert _logprob_call(lib, zeros, True, d=24577) == S["ALIGN"]
     assert _logprob_call(lib, None, False) == _logprob_call(lib, None, True) == S["NULL"]
+
+
+def _adamw_call(lib, ctx, n=1, how=None, **over):
+    import ctypes
+    from paper_2602_01469_b200 import binding
+    h = dict(lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, step=1, lr_dev=None, step_dev=None, grad_scale_dev=None, seed=0)
+    h.update(how or {})
+    t = dict(param=4096, grad=8192, master=None, m=12288, v=16384, m_scale=None, v_scale=None, count=10, param_dtype=1,
+             grad_dtype=1, weight_decay=0.0)
+    t.update(over)
+    arr = (binding.peagle_adamw_tensor_t * 1)(binding.peagle_adamw_tensor_t(**t))
+    return lib.peagle_adamw_step(ctx, ctypes.byref(binding.peagle_adamw_t(**h)), arr, n, ctypes.c_void_p(0))
+
+
+@pytest.mark.parametrize("how,over,status", [
+    ({"lr": -1.0}, {}, "BAD_SHAPE"), ({"lr": float("nan")}, {}, "BAD_SHAPE"), ({"beta1": 1.0}, {}, "BAD_SHAPE"),
+    ({"beta2": -0.1}, {}, "BAD_SHAPE"), ({"eps": 0.0}, {}, "BAD_SHAPE"), ({"step": 0}, {}, "BAD_SHAPE"),
+    ({"step_dev": 4}, {}, "ALIGN"), ({"lr_dev": 2}, {}, "ALIGN"), ({}, {"count": -1}, "BAD_SHAPE"),
+    ({}, {"param": None}, "NULL"), ({}, {"grad": None}, "NULL"), ({}, {"m": None}, "NULL"), ({}, {"v": None}, "NULL"),
+    ({}, {"param": 4097}, "ALIGN"), ({}, {"m": 12290}, "ALIGN"), ({}, {"param_dtype": 7}, "BAD_SHAPE"),
+    ({}, {"weight_decay": -0.1}, "BAD_SHAPE"), ({}, {"weight_decay": float("nan")}, "BAD_SHAPE"),
+    ({}, {"param_dtype": 0, "master": 4096}, "BAD_SHAPE"), ({}, {"m_scale": 4096}, "BAD_SHAPE"),
+    ({}, {"m_scale": 4098, "v_scale": 4096}, "ALIGN"), ({}, {"count": 1 << 41}, "TOO_LARGE"),
+])
+def test_adamw_refusals(lib, zeros, how, over, status):
+    from paper_2602_01469_b200 import binding
+    assert _adamw_call(lib, zeros, 1, how, **over) == binding.STATUS[status]
+
+
+def test_adamw_refuses_bad_lists(lib, zeros):
+    from paper_2602_01469_b200 import binding
+    import ctypes
+    S = binding.STATUS
+    assert _adamw_call(lib, zeros, -1) == S["BAD_SHAPE"]
+    assert _adamw_call(lib, None, 1) == S["NULL"]
+    assert lib.peagle_adamw_step(zeros, None, None, 0, None) == S["NULL"]
+    how = binding.peagle_adamw_t(1e-3, 0.9, 0.99, 1e-8, 1)
+    assert lib.peagle_adamw_step(zeros, ctypes.byref(how), None, 2, None) == S["NULL"]
