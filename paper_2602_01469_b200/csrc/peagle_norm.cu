@@ -43,12 +43,16 @@ __device__ __forceinline__ float load_w(const void *w, int dtype, int c, float a
 
 // ------------------------------------------------------------------ rows in registers
 
+// Threads of a block: whole groups.
+__host__ __device__ constexpr int block_threads(int tpr) { return tpr == 192 ? 384 : tpr < 256 ? 256 : tpr; }
+
 // What thread t of a group has of a row: E elements, in 16-byte pieces TPR pieces apart (VEC: base addresses and
 // row strides are multiples of 16 bytes), or single elements TPR apart.
 template <class T, bool VEC, int TPR, int E>
 struct Part {
     static constexpr int PIECE = VEC ? 16 / (int)sizeof(T) : 1;
     static constexpr int N = E / PIECE;
+    [[maybe_unused]] static constexpr int BT = block_threads(TPR);
     static constexpr bool PACKED = VEC && sizeof(T) == 2; // bf16 pairs stay packed
     static constexpr int WORDS = PACKED ? E / 2 : E;
     uint32_t raw[WORDS];
@@ -62,17 +66,26 @@ struct Part {
     }
 
     // Starts to fetch the share of a row, into the thread's own places in `stage` (shared memory, 16 bytes x threads
-    // for every piece); single elements are fetched when they are taken.  cols = 0: zeros.
+    // for every piece); single elements are fetched when they are taken.  `row` is the row's address plus t pieces.
     static __device__ __forceinline__ void fetch(const T *row, int t, int cols, uint32_t stage)
     {
         if constexpr (VEC) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) {
-                const int c = (n * TPR + t) * PIECE;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(stage + n * blockDim.x * 16),
-                             "l"(c < cols ? row + c : row), "r"(c < cols ? 16 : 0)
-                             : "memory");
-            }
+            for (int n = 0; n < N; ++n)
+                if ((n * TPR + t) * PIECE < cols)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage + n * BT * 16),
+                                 "l"(row + n * TPR * PIECE)
+                                 : "memory");
+        }
+    }
+    // Places past the last column are never fetched: zeros, once.
+    static __device__ __forceinline__ void clear(int t, int cols, uint4 *stage)
+    {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+                if ((n * TPR + t) * PIECE >= cols)
+                    stage[n * BT] = make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void take(const T *row, int t, int cols, const uint4 *stage)
@@ -80,16 +93,21 @@ struct Part {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if constexpr (VEC) {
-                const uint4 v = stage[n * blockDim.x];
+                const uint4 v = stage[n * BT];
                 raw[4 * n] = v.x;
                 raw[4 * n + 1] = v.y;
                 raw[4 * n + 2] = v.z;
                 raw[4 * n + 3] = v.w;
             } else {
-                const int c = n * TPR + t;
-                raw[n] = c < cols ? __float_as_uint(load1(row + c)) : 0u;
+                raw[n] = n * TPR + t < cols ? __float_as_uint(load1(row + n * TPR)) : 0u;
             }
         }
+    }
+    __device__ __forceinline__ void zero()
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i)
+            raw[i] = 0;
     }
     // What was made of the elements before is not kept in registers past here; the elements are.
     __device__ __forceinline__ void forget()
@@ -106,27 +124,40 @@ struct Part {
             return __uint_as_float(raw[e]);
     }
     // elements e and e + 1, e even
-    __device__ __forceinline__ void set2(int e, float a, float b)
+    __device__ __forceinline__ F2 get2(int e) const { return f2(get(e), get(e + 1)); }
+    __device__ __forceinline__ void set2(int e, F2 v)
     {
+        const float2 u = unf2(v);
         if constexpr (PACKED) {
-            raw[e / 2] = pack_bf16x2(a, b);
+            raw[e / 2] = pack_bf16x2(u.x, u.y);
         } else {
-            raw[e] = __float_as_uint(a);
-            raw[e + 1] = __float_as_uint(b);
+            raw[e] = __float_as_uint(u.x);
+            raw[e + 1] = __float_as_uint(u.y);
         }
     }
-    __device__ __forceinline__ void store(T *row, int t, int cols) const
+    // elements e to e + 3 of a row in shared memory, e a multiple of 4
+    static __device__ __forceinline__ void weights4(const float *sw, int t, int e, F2 &a, F2 &b)
+    {
+        if constexpr (VEC) {
+            const float4 w = *reinterpret_cast<const float4 *>(sw + place(t, e));
+            a = f2(w.x, w.y);
+            b = f2(w.z, w.w);
+        } else {
+            a = f2(sw[place(t, e)], sw[place(t, e + 1)]);
+            b = f2(sw[place(t, e + 2)], sw[place(t, e + 3)]);
+        }
+    }
+    __device__ __forceinline__ void store(T *row, int t, int cols) const // `row` as above
     {
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int c = (n * TPR + t) * PIECE;
-            if (c < cols) {
+        for (int n = 0; n < N; ++n)
+            if ((n * TPR + t) * PIECE < cols) {
                 if constexpr (VEC)
-                    *reinterpret_cast<uint4 *>(row + c) = make_uint4(raw[4 * n], raw[4 * n + 1], raw[4 * n + 2], raw[4 * n + 3]);
+                    *reinterpret_cast<uint4 *>(row + n * TPR * PIECE) =
+                        make_uint4(raw[4 * n], raw[4 * n + 1], raw[4 * n + 2], raw[4 * n + 3]);
                 else
-                    store1(row + c, __uint_as_float(raw[n]));
+                    store1(row + n * TPR, __uint_as_float(raw[n]));
             }
-        }
     }
 };
 
@@ -142,121 +173,174 @@ __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_
 template <int LEFT>
 __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(LEFT) : "memory"); }
 
-// Threads of a block: whole groups.
-__host__ __device__ constexpr int block_threads(int tpr) { return tpr == 192 ? 384 : tpr < 256 ? 256 : tpr; }
 
 // Sums over the threads of a group.  `red` has two halves that take turns, so that one barrier is enough.
 template <int TPR>
-__device__ __forceinline__ float2 group_sum(float a, float b, float2 (*red)[block_threads(TPR) / 32], int &turn)
+__device__ __forceinline__ float group_sum(float a, float (*red)[block_threads(TPR) / 32], int &turn)
+{
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1)
+        a += __shfl_xor_sync(~0u, a, o);
+    if constexpr (TPR > 32) {
+        constexpr int W = TPR / 32;
+        const int warp = threadIdx.x >> 5, group = warp / W;
+        if ((threadIdx.x & 31) == 0)
+            red[turn][warp] = a;
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
+        a = 0.f;
+#pragma unroll
+        for (int i = 0; i < W; ++i)
+            a += red[turn][group * W + i];
+        turn ^= 1;
+    }
+    return a;
+}
+template <int TPR>
+__device__ __forceinline__ float2 group_sum2(F2 v, float2 (*red)[block_threads(TPR) / 32], int &turn)
 {
 #pragma unroll
     for (int o = (TPR < 32 ? TPR : 32) / 2; o; o >>= 1) {
-        a += __shfl_xor_sync(~0u, a, o);
-        b += __shfl_xor_sync(~0u, b, o);
+        const float2 u = unf2(v);
+        v = add_f2(v, f2(__shfl_xor_sync(~0u, u.x, o), __shfl_xor_sync(~0u, u.y, o)));
     }
     if constexpr (TPR > 32) {
         constexpr int W = TPR / 32;
         const int warp = threadIdx.x >> 5, group = warp / W;
         if ((threadIdx.x & 31) == 0)
-            red[turn][warp] = make_float2(a, b);
+            red[turn][warp] = unf2(v);
         asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
-        a = b = 0.f;
+        v = f2(0.f, 0.f);
 #pragma unroll
         for (int i = 0; i < W; ++i) {
-            const float2 v = red[turn][group * W + i];
-            a += v.x;
-            b += v.y;
+            const float2 u = red[turn][group * W + i];
+            v = add_f2(v, f2(u.x, u.y));
         }
         turn ^= 1;
     }
-    return make_float2(a, b);
+    return unf2(v);
 }
 
 // Blocks that an SM should hold: about 768 threads; 512 where a thread holds 48 words of elements and sums or more.
 constexpr int blocks_per_sm(int threads, int words) { return threads >= 512 ? 1 : (words >= 48 ? 512 : 768) / threads; }
 
-template <class T, bool VEC, int TPR, int E>
-__global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const NormArgs a)
+// Weights as fp32 in shared memory: group g brings every G-th element of each thread's share; zeros past the end.
+template <class Row, int E, int G>
+__device__ __forceinline__ void stage_weights(float *to, const void *w, int dtype, float absent, int t, int g, int cols)
 {
-    using Row = Part<T, VEC, TPR, E>;
-    using Stages = Ring<T, VEC, TPR, E, 1>;
-    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH;
-    extern __shared__ float4 smem[];
-    uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
-    float *sw = reinterpret_cast<float *>(smem + D * Stages::PIECES * BT), *sb = sw + TPR * E;
-    __shared__ float2 red[2][BT / 32];
-    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
-    const bool layer = a.kind == PEAGLE_NORM_LAYER;
-    const T *X = static_cast<const T *>(a.X);
-    const int64_t step = (int64_t)gridDim.x * G;
-    const int64_t first = (int64_t)blockIdx.x * G + g;
-    const uint32_t ring_at = smem_u32(ring);
-#pragma unroll
-    for (int i = 0; i < D; ++i) {
-        const int64_t r = first + i * step;
-        Row::fetch(r < a.rows ? X + r * a.ldx : X, t, r < a.rows ? a.cols : 0, ring_at + i * Stages::PIECES * BT * 16);
-        copies_commit();
-    }
-    // group g brings every G-th element of each thread's share
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const int c = Row::col(t, e);
-        if (e % G == g && c < a.cols) {
-            sw[Row::place(t, e)] = load_w(a.weight, a.w_dtype, c, 1.f);
-            if (a.bias)
-                sb[Row::place(t, e)] = load_w(a.bias, a.w_dtype, c, 0.f);
-        }
+        if (e % G == g)
+            to[Row::place(t, e)] = c < cols ? load_w(w, dtype, c, absent) : 0.f;
     }
+}
+
+template <class T, bool VEC, int TPR, int E>
+__global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __grid_constant__ NormArgs a)
+{
+    using Row = Part<T, VEC, TPR, E>;
+    using Stages = Ring<T, VEC, TPR, E, 1>;
+    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::PIECES * BT;
+    extern __shared__ float4 smem[];
+    uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
+    float *sw = reinterpret_cast<float *>(smem + D * STAGE), *sb = sw + TPR * E;
+    __shared__ float red1[2][BT / 32];
+    __shared__ float2 red2[2][BT / 32];
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
+    const bool layer = a.kind == PEAGLE_NORM_LAYER;
+    const uint32_t rows = a.rows, step = gridDim.x * G, first = blockIdx.x * G + g;
+    const T *x_at = static_cast<const T *>(a.X) + first * a.ldx + t * Row::PIECE; // the row at hand
+    T *y_at = static_cast<T *>(a.Y) + first * a.ldy + t * Row::PIECE;
+    const int64_t x_step = step * a.ldx, y_step = step * a.ldy;
+    uint32_t ring_at = smem_u32(ring);
+#pragma unroll
+    for (int i = 0; i < D; ++i) {
+        Row::clear(t, cols, ring + i * STAGE);
+        if (first + i * step < rows)
+            Row::fetch(x_at + i * x_step, t, cols, ring_at + i * STAGE * 16);
+        copies_commit();
+    }
+    stage_weights<Row, E, G>(sw, a.weight, a.w_dtype, 1.f, t, g, cols);
+    if (a.bias)
+        stage_weights<Row, E, G>(sb, a.bias, a.w_dtype, 0.f, t, g, cols);
     __syncthreads();
-    const float n = (float)a.cols;
+    const float n = (float)cols;
     int turn = 0, stage = 0;
-    for (int64_t r = first; r - g < a.rows; r += step) {
-        const bool live = r < a.rows;
+    // groups of less than a warp stay together with their warp
+    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows; r += step, x_at += x_step, y_at += y_step) {
         Row x;
         copies_wait<D - 1>();
-        x.take(X + r * a.ldx, t, live ? a.cols : 0, ring + stage * Stages::PIECES * BT);
-        float mu = 0.f;
+        if (VEC || r < rows)
+            x.take(x_at, t, cols, ring + stage * STAGE);
+        float mu = 0.f, var;
         if (layer) {
-            float s = 0.f;
+            F2 s = f2(0.f, 0.f), q = s;
 #pragma unroll
-            for (int e = 0; e < E; ++e)
-                s += x.get(e);
-            mu = group_sum<TPR>(s, 0.f, red, turn).x / n;
-        }
-        float s = 0.f, q = 0.f;
+            for (int e = 0; e < E; e += 2)
+                s = add_f2(s, x.get2(e));
+            const float2 sum = unf2(s);
+            mu = group_sum<TPR>(sum.x + sum.y, red1, turn) / n;
+            const F2 minus = f2(-mu, -mu);
+            s = q;
 #pragma unroll
-        for (int e = 0; e < E; ++e)
-            if (Row::col(t, e) < a.cols) {
-                const float d = x.get(e) - mu;
-                s += d;
-                q = fmaf(d, d, q);
+            for (int e = 0; e < E; e += 2) {
+                F2 d = add_f2(x.get2(e), minus);
+                if (!VEC && Row::col(t, e) >= cols)
+                    d = f2(0.f, 0.f);
+                else if (!VEC && Row::col(t, e + 1) >= cols)
+                    d = f2(unf2(d).x, 0.f);
+                if (!VEC || Row::col(t, e) < cols) {
+                    s = add_f2(s, d);
+                    q = fma_f2(d, d, q);
+                }
             }
-        const float2 sq = group_sum<TPR>(s, q, red, turn);
+            const float2 s2 = unf2(s), q2 = unf2(q);
+            const float2 both = group_sum2<TPR>(f2(s2.x + s2.y, q2.x + q2.y), red2, turn);
+            const float left = both.x / n; // the rounding of mu is taken out of both
+            mu += left;
+            var = both.y / n - left * left;
+        } else {
+            F2 q = f2(0.f, 0.f);
+#pragma unroll
+            for (int e = 0; e < E; e += 2)
+                q = fma_f2(x.get2(e), x.get2(e), q);
+            const float2 q2 = unf2(q);
+            var = group_sum<TPR>(q2.x + q2.y, red1, turn) / n;
+        }
         // the sums are formed, so the stage has been read
-        const int64_t ahead = r + D * step;
-        Row::fetch(ahead < a.rows ? X + ahead * a.ldx : X, t, ahead < a.rows ? a.cols : 0,
-                   ring_at + stage * Stages::PIECES * BT * 16);
+        if (r + D * step < rows)
+            Row::fetch(x_at + D * x_step, t, cols, ring_at + stage * STAGE * 16);
         copies_commit();
-        stage = stage + 1 == D ? 0 : stage + 1;
-        // the rounding of mu is taken out of both
-        const float left = layer ? sq.x / n : 0.f;
-        mu += left;
-        const float var = sq.y / n - left * left;
+        if (D > 1)
+            stage ^= 1;
         const float rstd = rsqrtf((var < 0.f ? 0.f : var) + a.eps); // a NaN stays one
+        const F2 minus = f2(-mu, -mu), by = f2(rstd, rstd);
+        x.forget();
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            float v[2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = Row::place(t, e + k);
-                v[k] = (x.get(e + k) - mu) * rstd * sw[at];
-                if (a.bias)
-                    v[k] += sb[at];
+        for (int e = 0; e < E; e += 4) {
+            F2 w0, w1;
+            Row::weights4(sw, t, e, w0, w1);
+            F2 v0 = x.get2(e), v1 = x.get2(e + 2);
+            if (layer) {
+                v0 = add_f2(v0, minus);
+                v1 = add_f2(v1, minus);
             }
-            x.set2(e, v[0], v[1]);
+            v0 = mul_f2(v0, by);
+            v1 = mul_f2(v1, by);
+            if (a.bias) {
+                F2 b0, b1;
+                Row::weights4(sb, t, e, b0, b1);
+                v0 = fma_f2(v0, w0, b0);
+                v1 = fma_f2(v1, w1, b1);
+            } else {
+                v0 = mul_f2(v0, w0);
+                v1 = mul_f2(v1, w1);
+            }
+            x.set2(e, v0);
+            x.set2(e + 2, v1);
         }
-        if (live) {
-            x.store(static_cast<T *>(a.Y) + r * a.ldy, t, a.cols);
+        if (r < rows) {
+            x.store(y_at, t, cols);
             if (t == 0) {
                 if (a.mean)
                     a.mean[r] = mu;
@@ -271,132 +355,155 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const Norm
 template <class T, bool VEC, int TPR, int E, int SUMS>
 __global__ void __launch_bounds__(block_threads(TPR),
                                   blocks_per_sm(block_threads(TPR), 2 * Part<T, VEC, TPR, E>::WORDS + SUMS * E))
-    norm_bwd_kernel(const NormArgs a)
+    norm_bwd_kernel(const __grid_constant__ NormArgs a)
 {
     using Row = Part<T, VEC, TPR, E>;
     using Stages = Ring<T, VEC, TPR, E, 2>;
-    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, HALF = Stages::PIECES / 2;
+    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::PIECES * BT, HALF = STAGE / 2;
     extern __shared__ float4 smem[];
     uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
-    float *sw = reinterpret_cast<float *>(smem + D * Stages::PIECES * BT);
+    float *sw = reinterpret_cast<float *>(smem + D * STAGE);
     __shared__ float2 red[2][BT / 32];
-    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR;
+    const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
     const bool layer = a.kind == PEAGLE_NORM_LAYER;
-    const T *X = static_cast<const T *>(a.X), *DY = static_cast<const T *>(a.dY);
-    const int64_t step = (int64_t)gridDim.x * G;
-    const int64_t first = (int64_t)blockIdx.x * G + g;
+    const uint32_t rows = a.rows, step = gridDim.x * G, first = blockIdx.x * G + g;
+    const T *x_at = static_cast<const T *>(a.X) + first * a.ldx + t * Row::PIECE;
+    const T *dy_at = static_cast<const T *>(a.dY) + first * a.lddy + t * Row::PIECE;
+    T *dx_at = static_cast<T *>(a.dX) + first * a.lddx + t * Row::PIECE;
+    const int64_t x_step = step * a.ldx, dy_step = step * a.lddy, dx_step = step * a.lddx;
     const uint32_t ring_at = smem_u32(ring);
-    const auto fetch = [&](int64_t r, int stage) {
-        const bool live = r < a.rows;
-        const uint32_t at = ring_at + stage * Stages::PIECES * BT * 16;
-        Row::fetch(live ? X + r * a.ldx : X, t, live ? a.cols : 0, at);
-        Row::fetch(live ? DY + r * a.lddy : DY, t, live ? a.cols : 0, at + HALF * BT * 16);
-        copies_commit();
-    };
 #pragma unroll
-    for (int i = 0; i < D; ++i)
-        fetch(first + i * step, i);
+    for (int i = 0; i < D; ++i) {
+        Row::clear(t, cols, ring + i * STAGE);
+        Row::clear(t, cols, ring + i * STAGE + HALF);
+        if (first + i * step < rows) {
+            Row::fetch(x_at + i * x_step, t, cols, ring_at + i * STAGE * 16);
+            Row::fetch(dy_at + i * dy_step, t, cols, ring_at + (i * STAGE + HALF) * 16);
+        }
+        copies_commit();
+    }
     float mu = 0.f, rstd = 0.f; // of the row to come
-    if (first < a.rows) {
+    if (first < rows) {
         mu = layer ? a.mean_in[first] : 0.f;
         rstd = a.rstd_in[first];
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const int c = Row::col(t, e);
-        if (e % G == g)
-            sw[Row::place(t, e)] = c < a.cols ? load_w(a.weight, a.w_dtype, c, 1.f) : 0.f;
-    }
+    stage_weights<Row, E, G>(sw, a.weight, a.w_dtype, 1.f, t, g, cols);
     __syncthreads();
-    float dw[SUMS > 0 ? E : 1], db[SUMS > 1 ? E : 1];
+    F2 dw[SUMS > 0 ? E / 2 : 1], db[SUMS > 1 ? E / 2 : 1];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < E / 2; ++e) {
         if (SUMS > 0)
-            dw[e] = 0.f;
+            dw[e] = f2(0.f, 0.f);
         if (SUMS > 1)
-            db[e] = 0.f;
+            db[e] = f2(0.f, 0.f);
     }
-    const float n = (float)a.cols;
+    const float n = (float)cols;
     int turn = 0, stage = 0;
-    for (int64_t r = first; r - g < a.rows; r += step) {
-        const bool live = r < a.rows;
+    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows;
+         r += step, x_at += x_step, dy_at += dy_step, dx_at += dx_step) {
         Row x, dy;
-        const float m = mu, rs = rstd;
-        mu = rstd = 0.f;
-        if (r + step < a.rows) {
+        const F2 minus = f2(-mu, -mu), by = f2(rstd, rstd);
+        const float rs = rstd;
+        if (r + step < rows) {
             mu = layer ? a.mean_in[r + step] : 0.f;
             rstd = a.rstd_in[r + step];
         }
         copies_wait<D - 1>();
-        x.take(X + r * a.ldx, t, live ? a.cols : 0, ring + stage * Stages::PIECES * BT);
-        dy.take(DY + r * a.lddy, t, live ? a.cols : 0, ring + (stage * Stages::PIECES + HALF) * BT);
-        float s0 = 0.f, s1 = 0.f; // columns past the last have dy = w = 0
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float d = dy.get(e), xh = (x.get(e) - m) * rs, u = d * sw[Row::place(t, e)];
-            s0 += u;
-            s1 = fmaf(u, xh, s1);
-            if (SUMS > 0)
-                dw[e] = fmaf(d, xh, dw[e]);
-            if (SUMS > 1)
-                db[e] += d;
+        if (VEC || r < rows) {
+            x.take(x_at, t, cols, ring + stage * STAGE);
+            dy.take(dy_at, t, cols, ring + stage * STAGE + HALF);
         }
-        const float2 s = group_sum<TPR>(s0, s1, red, turn);
-        fetch(r + D * step, stage); // the sums are formed, so the stage has been read
-        stage = stage + 1 == D ? 0 : stage + 1;
-        const float c0 = layer ? s.x / n : 0.f, c1 = s.y / n;
+        if (TPR < 32 && r >= rows) {
+            x.zero();
+            dy.zero();
+        }
+        F2 s0 = f2(0.f, 0.f), s1 = s0; // columns past the last have dy = w = 0
+#pragma unroll
+        for (int e = 0; e < E; e += 4) {
+            F2 w[2];
+            Row::weights4(sw, t, e, w[0], w[1]);
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const F2 d = dy.get2(e + 2 * k), xh = mul_f2(add_f2(x.get2(e + 2 * k), minus), by), u = mul_f2(d, w[k]);
+                s0 = add_f2(s0, u);
+                s1 = fma_f2(u, xh, s1);
+                if (SUMS > 0)
+                    dw[e / 2 + k] = fma_f2(d, xh, dw[e / 2 + k]);
+                if (SUMS > 1)
+                    db[e / 2 + k] = add_f2(db[e / 2 + k], d);
+            }
+        }
+        const float2 p0 = unf2(s0), p1 = unf2(s1);
+        const float2 s = group_sum2<TPR>(f2(p0.x + p0.y, p1.x + p1.y), red, turn);
+        // the sums are formed, so the stage has been read
+        if (r + D * step < rows) {
+            Row::fetch(x_at + D * x_step, t, cols, ring_at + stage * STAGE * 16);
+            Row::fetch(dy_at + D * dy_step, t, cols, ring_at + (stage * STAGE + HALF) * 16);
+        }
+        copies_commit();
+        if (D > 1)
+            stage ^= 1;
+        const float c0 = layer ? -rs * (s.x / n) : 0.f, c1 = -rs * (s.y / n);
         x.forget();
         dy.forget();
 #pragma unroll
-        for (int e = 0; e < E; e += 2) {
-            float v[2];
+        for (int e = 0; e < E; e += 4) {
+            F2 w[2];
+            Row::weights4(sw, t, e, w[0], w[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const float u = dy.get(e + k) * sw[Row::place(t, e + k)], xh = (x.get(e + k) - m) * rs;
-                v[k] = rs * (u - c0 - xh * c1);
+                const F2 u = mul_f2(dy.get2(e + 2 * k), w[k]), xh = mul_f2(add_f2(x.get2(e + 2 * k), minus), by);
+                x.set2(e + 2 * k, fma_f2(xh, f2(c1, c1), fma_f2(u, by, f2(c0, c0))));
             }
-            x.set2(e, v[0], v[1]);
         }
-        if (live)
-            x.store(static_cast<T *>(a.dX) + r * a.lddx, t, a.cols);
+        if (r < rows)
+            x.store(dx_at, t, cols);
     }
     copies_wait<0>();
     pdl_trigger(); // the kernel that joins the blocks may settle down
     if constexpr (SUMS > 0) {
 #pragma unroll
         for (int which = 0; which < SUMS; ++which) {
-            __syncthreads(); // weights, and the sums before, have been read
-            if (G > 1) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    sw[(g * E + e) * TPR + t] = which ? db[e] : dw[e];
-                __syncthreads();
-            }
             float *out = which ? a.db : a.dw;
-            float *part = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * a.cols;
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const int c = Row::col(t, e);
-                if (e % G != g || c >= a.cols)
-                    continue;
-                float v = which ? db[e] : dw[e];
-                if (G > 1) {
-                    v = 0.f;
-#pragma unroll
-                    for (int k = 0; k < G; ++k)
-                        v += sw[(k * E + e) * TPR + t];
-                }
+            float *part = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * cols;
+            const auto mine = [&](int e) {
+                const float2 v = unf2(which ? db[SUMS > 1 ? e / 2 : 0] : dw[e / 2]);
+                return e & 1 ? v.y : v.x;
+            };
+            const auto leave = [&](int c, float v) {
                 if (gridDim.x > 1)
                     part[c] = v;
                 else if (out)
                     out[c] += v;
+            };
+            if (G == 1) {
+#pragma unroll
+                for (int e = 0; e < E; ++e)
+                    if (Row::col(t, e) < cols)
+                        leave(Row::col(t, e), mine(e));
+                continue;
+            }
+            __syncthreads(); // weights, and the sums before, have been read
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                sw[(g * E + e) * TPR + t] = mine(e);
+            __syncthreads();
+            for (int i = threadIdx.x; i < TPR * E; i += BT) {
+                const int c = Row::col(i % TPR, i / TPR);
+                if (c >= cols)
+                    continue;
+                float v = 0.f;
+#pragma unroll
+                for (int k = 0; k < G; ++k)
+                    v += sw[k * E * TPR + i];
+                leave(c, v);
             }
         }
     }
 }
 
 // Adds the parts' column sums to dw and db: 32 columns to a block, a part to every 32nd row of threads.
-__global__ void __launch_bounds__(1024) norm_bwd_join(const NormArgs a, int parts)
+__global__ void __launch_bounds__(1024) norm_bwd_join(const __grid_constant__ NormArgs a, int parts)
 {
     pdl_wait();
     __shared__ float s[32][33];
