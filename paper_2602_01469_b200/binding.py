@@ -80,6 +80,21 @@ class peagle_adamw_t(ctypes.Structure):
     ]
 
 
+def _argtypes(letters):
+    """p: pointer, i: int32, l: int64, f: float."""
+    kinds = {"p": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float}
+    return [kinds[c] for c in letters]
+
+
+# Entry points that short calls go through: with their types known, ctypes takes plain numbers.
+_ARGTYPES = {
+    "peagle_norm_fwd": _argtypes("piiiiiplppfplppp"),
+    "peagle_norm_bwd": _argtypes("piiiiiplpppplplppp"),
+    "peagle_token_logprobs_fwd": _argtypes("piiiplpfpppippp"),
+    "peagle_token_logprobs_bwd": _argtypes("piiiplpfpppppl") + [ctypes.c_void_p],
+    "peagle_adamw_step": _argtypes("pppip"),
+}
+
 _lib = None
 
 
@@ -96,6 +111,8 @@ def lib():
         L.peagle_last_cuda_error.argtypes = [ctypes.c_void_p]
         L.peagle_launch_count.restype = ctypes.c_int64
         L.peagle_launch_count.argtypes = [ctypes.c_void_p]
+        for name, types in _ARGTYPES.items():
+            getattr(L, name).argtypes = types
         _lib = L
     return _lib
 
@@ -132,44 +149,61 @@ def _stream(stream):
     return ctypes.c_void_p(int(stream))
 
 
+# ---- arguments of the operators around the layer.  Their calls can be as short as a few microseconds on the GPU, so
+# the checks ask a tensor as little as they can.
+
+def _current_stream(device):
+    import torch
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+def _know_torch():
+    global _current_stream
+    import torch
+    # the same without the Python object around the handle, 0.1 instead of 1.3 us, where torch has it
+    _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _current_stream)
+    _dtypes.update({torch.float32: 0, torch.bfloat16: 1})
+    _f32[:], _i32[:], _i64[:] = [torch.float32], [torch.int32], [torch.int64]
+
+
+def _refuse(status="BAD_SHAPE"):
+    raise PeagleError(STATUS[status])
+
+
 def _stream_on(ctx, stream):
-    """Like ``_stream``; without one, the current stream of the context's own device."""
+    """The stream's handle; without one, the current stream of the context's own device."""
     if stream is None:
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream(ctx.device).cuda_stream)
-    return _stream(stream)
+        return _current_stream(ctx.device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+_dtypes = {}                       # peagle_dtype by torch dtype
+_f32, _i32, _i64 = [], [], []      # the torch dtypes of vectors; filled, like _dtypes, when torch is there
 
 
 def _dtype(t):
     """peagle_dtype of a tensor."""
-    import torch
-    if t.dtype == torch.float32:
-        return 0
-    if t.dtype == torch.bfloat16:
-        return 1
-    raise PeagleError(STATUS["BAD_SHAPE"])
+    code = _dtypes.get(t.dtype)
+    return code if code is not None else _refuse()
 
 
-def _require(ok, status="BAD_SHAPE"):
-    if not ok:
-        raise PeagleError(STATUS[status])
+def _matrix(t, rows, cols, dtype, device):
+    """Address and leading dimension of a [rows, cols] tensor on the context's device whose rows are contiguous."""
+    if t.shape != (rows, cols) or t.dtype != dtype or t.get_device() != device:
+        _refuse()
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        _refuse()
+    return t.data_ptr(), ld if rows != 1 else max(ld, cols)
 
 
-def _on(ctx, *tensors):
-    """Every tensor that is given lies on the context's device."""
-    for t in tensors:
-        _require(t is None or (t.is_cuda and t.device.index == ctx.device))
-
-
-def _ld(t, rows, cols):
-    """Leading dimension of a [rows, cols] tensor whose rows are contiguous."""
-    _require(t.dim() == 2 and tuple(t.shape) == (rows, cols) and (cols == 1 or t.stride(1) == 1))
-    return ctypes.c_int64(max(t.stride(0), cols) if rows == 1 else t.stride(0))
-
-
-def _vector(t, n, *dtypes):
-    """A contiguous vector of n elements, or none."""
-    _require(t is None or (t.dim() == 1 and t.shape[0] == n and (n <= 1 or t.stride(0) == 1) and t.dtype in dtypes))
+def _vector(t, n, dtypes, device):
+    """Address of a contiguous vector of n elements, None of none."""
+    if t is None:
+        return None
+    if t.shape != (n,) or t.dtype not in dtypes or t.get_device() != device or not t.is_contiguous():
+        _refuse()
+    return t.data_ptr()
 
 
 class Problem:
@@ -220,6 +254,7 @@ class AdamWTensors:
 
     def __init__(self, items):
         import torch
+        _know_torch()
         self.items = [dict(i) for i in items]
         self.device = self.items[0]["param"].device.index if self.items else None
         self.c = (peagle_adamw_tensor_t * max(len(self.items), 1))()
@@ -233,31 +268,34 @@ class AdamWTensors:
                                        ("v_scale", torch.float32, -(-n // ADAMW_BLOCK))):
                 t = i.get(name)
                 if t is None:
-                    _require(name == "master" or (name.endswith("scale") and not eight))
+                    if not (name == "master" or (name.endswith("scale") and not eight)):
+                        _refuse()
                     continue
-                _require(t.dtype == dtype and t.numel() == count and t.is_contiguous())
-                self._own(t)
+                self._own(t, count)
+                if t.dtype != dtype:
+                    _refuse()
                 written.append((t.data_ptr(), t.numel() * t.element_size()))
                 setattr(c, name, t.data_ptr())
-            _require(p.is_contiguous())
-            self._own(p)
+            self._own(p, n)
             written.append((p.data_ptr(), n * p.element_size()))
             c.param, c.count, c.param_dtype = p.data_ptr(), n, _dtype(p)
             c.weight_decay = float(i.get("weight_decay", 0.0))
         written = sorted(w for w in written if w[1])
-        _require(all(a + size <= b for (a, size), (b, _) in zip(written, written[1:])), "BAD_RANGE")
+        if any(a + size > b for (a, size), (b, _) in zip(written, written[1:])):
+            _refuse("BAD_RANGE")
         self.set_grads([i["grad"] for i in self.items])
 
-    def _own(self, t):
-        _require(t.is_cuda and t.device.index == self.device)
+    def _own(self, t, count):
+        if not t.is_cuda or t.get_device() != self.device or t.numel() != count or not t.is_contiguous():
+            _refuse()
 
     def set_grads(self, grads):
         """Other gradients for the steps to come, in the order of the tensors."""
         grads = list(grads)
-        _require(len(grads) == len(self.items))
+        if len(grads) != len(self.items):
+            _refuse()
         for c, i, g in zip(self.c, self.items, grads):
-            _require(g.numel() == c.count and g.is_contiguous())
-            self._own(g)
+            self._own(g, c.count)
             c.grad, c.grad_dtype = g.data_ptr(), _dtype(g)
             i["grad"] = g
 
@@ -266,6 +304,7 @@ class Context:
     def __init__(self, device: int = 0):
         self.h = ctypes.c_void_p()
         self.device = int(device)
+        _know_torch()
         _check(lib().peagle_create(ctypes.byref(self.h), int(device)))
 
     def close(self):
@@ -391,91 +430,93 @@ def peagle_layer_partitioned(ctx, prob: Problem, parts, X, W, rope_base, dO, O, 
 def peagle_norm_fwd(ctx, kind, X, weight, bias, eps, Y, mean=None, rstd=None, stream=None):
     """Layer norm (``NORM["layer"]``) or RMS norm (``NORM["rms"]``) of the rows of X into Y; weight, bias, and
     the fp32 statistics mean and rstd may be None.  Device tensors; rows of X and Y may lie apart."""
-    import torch
-    _require(X.dim() == 2)
+    if X.dim() != 2:
+        _refuse()
     rows, cols = X.shape
+    dtype, dev = _dtype(X), ctx.device
     w = weight if weight is not None else bias
-    _require(Y.dtype == X.dtype and (weight is None or bias is None or weight.dtype == bias.dtype))
-    for t in (weight, bias):
-        _vector(t, cols, torch.float32, torch.bfloat16)
-    for t in (mean, rstd):
-        _vector(t, rows, torch.float32)
-    _on(ctx, X, weight, bias, Y, mean, rstd)
-    _check(lib().peagle_norm_fwd(ctx.h, int(kind), _dtype(X), _dtype(w) if w is not None else 0, int(rows), int(cols),
-                                 _ptr(X), _ld(X, rows, cols), _ptr(weight), _ptr(bias), ctypes.c_float(eps), _ptr(Y),
-                                 _ld(Y, rows, cols), _ptr(mean), _ptr(rstd), _stream_on(ctx, stream)), ctx.h)
+    w_dtype = _dtype(w) if w is not None else 0
+    if bias is not None and bias.dtype != w.dtype:
+        _refuse()
+    x, ldx = _matrix(X, rows, cols, X.dtype, dev)
+    y, ldy = _matrix(Y, rows, cols, X.dtype, dev)
+    rc = lib().peagle_norm_fwd(ctx.h, kind, dtype, w_dtype, rows, cols, x, ldx, _vector(weight, cols, _dtypes, dev),
+                               _vector(bias, cols, _dtypes, dev), eps, y, ldy, _vector(mean, rows, _f32, dev),
+                               _vector(rstd, rows, _f32, dev), _stream_on(ctx, stream))
+    if rc:
+        _check(rc, ctx.h)
 
 
 def peagle_norm_bwd(ctx, kind, X, weight, mean, rstd, dY, dX, dweight_acc=None, dbias_acc=None, stream=None):
     """Backward of the norm: dX, and the gradients of weight and bias ADDED to fp32 sums."""
-    import torch
-    _require(X.dim() == 2)
+    if X.dim() != 2:
+        _refuse()
     rows, cols = X.shape
-    _require(dY.dtype == X.dtype and dX.dtype == X.dtype)
-    _vector(weight, cols, torch.float32, torch.bfloat16)
-    for t in (mean, rstd):
-        _vector(t, rows, torch.float32)
-    for t in (dweight_acc, dbias_acc):
-        _vector(t, cols, torch.float32)
-    _on(ctx, X, weight, mean, rstd, dY, dX, dweight_acc, dbias_acc)
-    _check(lib().peagle_norm_bwd(ctx.h, int(kind), _dtype(X), _dtype(weight) if weight is not None else 0, int(rows),
-                                 int(cols), _ptr(X), _ld(X, rows, cols), _ptr(weight), _ptr(mean), _ptr(rstd), _ptr(dY),
-                                 _ld(dY, rows, cols), _ptr(dX), _ld(dX, rows, cols), _ptr(dweight_acc), _ptr(dbias_acc),
-                                 _stream_on(ctx, stream)), ctx.h)
+    dtype, dev = _dtype(X), ctx.device
+    w_dtype = _dtype(weight) if weight is not None else 0
+    x, ldx = _matrix(X, rows, cols, X.dtype, dev)
+    dy, lddy = _matrix(dY, rows, cols, X.dtype, dev)
+    dx, lddx = _matrix(dX, rows, cols, X.dtype, dev)
+    rc = lib().peagle_norm_bwd(ctx.h, kind, dtype, w_dtype, rows, cols, x, ldx, _vector(weight, cols, _dtypes, dev),
+                               _vector(mean, rows, _f32, dev), _vector(rstd, rows, _f32, dev), dy, lddy, dx, lddx,
+                               _vector(dweight_acc, cols, _f32, dev), _vector(dbias_acc, cols, _f32, dev),
+                               _stream_on(ctx, stream))
+    if rc:
+        _check(rc, ctx.h)
 
 
 def peagle_token_logprobs_fwd(ctx, logits, tokens, scale=1.0, logprob=None, lse=None, entropy=None, top_logprobs=None,
                               top_ids=None, stream=None):
     """Log probability of ``tokens`` (int32, -1 for none) under the rows of ``logits``, with log-sum-exp, entropy
     and the top alternatives; every output may be None.  The width of the top outputs says how many."""
-    import torch
-    _require(logits.dim() == 2)
+    if logits.dim() != 2 or (top_logprobs is None) != (top_ids is None):
+        _refuse()
     rows, vocab = logits.shape
-    _vector(tokens, rows, torch.int32)
-    for t in (logprob, lse, entropy):
-        _vector(t, rows, torch.float32)
-    _require((top_logprobs is None) == (top_ids is None))
-    k = 0
+    dtype, dev = _dtype(logits), ctx.device
+    x, ld = _matrix(logits, rows, vocab, logits.dtype, dev)
+    k, top, ids = 0, None, None
     if top_ids is not None:
-        _require(top_ids.dim() == 2 and top_ids.shape == top_logprobs.shape and top_ids.shape[0] == rows and
-                 top_ids.dtype == torch.int32 and top_logprobs.dtype == torch.float32 and
-                 top_ids.is_contiguous() and top_logprobs.is_contiguous())
-        k = top_ids.shape[1]
-    _on(ctx, logits, tokens, logprob, lse, entropy, top_logprobs, top_ids)
-    _check(lib().peagle_token_logprobs_fwd(ctx.h, _dtype(logits), int(rows), int(vocab), _ptr(logits),
-                                           _ld(logits, rows, vocab), _ptr(tokens), ctypes.c_float(scale), _ptr(logprob),
-                                           _ptr(lse), _ptr(entropy), int(k), _ptr(top_logprobs), _ptr(top_ids),
-                                           _stream_on(ctx, stream)), ctx.h)
+        if top_ids.dim() != 2 or not top_ids.is_contiguous() or not top_logprobs.is_contiguous():
+            _refuse()
+        k = top_ids.size(1)
+        top = _matrix(top_logprobs, rows, k, _f32[0], dev)[0]
+        ids = _matrix(top_ids, rows, k, _i32[0], dev)[0]
+    rc = lib().peagle_token_logprobs_fwd(ctx.h, dtype, rows, vocab, x, ld, _vector(tokens, rows, _i32, dev), scale,
+                                         _vector(logprob, rows, _f32, dev), _vector(lse, rows, _f32, dev),
+                                         _vector(entropy, rows, _f32, dev), k, top, ids, _stream_on(ctx, stream))
+    if rc:
+        _check(rc, ctx.h)
 
 
 def peagle_token_logprobs_bwd(ctx, logits, tokens, scale, lse, entropy, g_logprob, g_entropy, dlogits, stream=None):
     """Gradient of the logits from those of logprob and entropy (either may be None); ``dlogits`` may be ``logits``."""
-    import torch
-    _require(logits.dim() == 2)
+    if logits.dim() != 2:
+        _refuse()
     rows, vocab = logits.shape
-    _require(dlogits.dtype == logits.dtype)
-    _vector(tokens, rows, torch.int32)
-    for t in (lse, entropy, g_logprob, g_entropy):
-        _vector(t, rows, torch.float32)
-    _on(ctx, logits, tokens, lse, entropy, g_logprob, g_entropy, dlogits)
-    _check(lib().peagle_token_logprobs_bwd(ctx.h, _dtype(logits), int(rows), int(vocab), _ptr(logits),
-                                           _ld(logits, rows, vocab), _ptr(tokens), ctypes.c_float(scale), _ptr(lse),
-                                           _ptr(entropy), _ptr(g_logprob), _ptr(g_entropy), _ptr(dlogits),
-                                           _ld(dlogits, rows, vocab), _stream_on(ctx, stream)), ctx.h)
+    dtype, dev = _dtype(logits), ctx.device
+    x, ld = _matrix(logits, rows, vocab, logits.dtype, dev)
+    d, ldd = _matrix(dlogits, rows, vocab, logits.dtype, dev)
+    rc = lib().peagle_token_logprobs_bwd(ctx.h, dtype, rows, vocab, x, ld, _vector(tokens, rows, _i32, dev), scale,
+                                         _vector(lse, rows, _f32, dev), _vector(entropy, rows, _f32, dev),
+                                         _vector(g_logprob, rows, _f32, dev), _vector(g_entropy, rows, _f32, dev), d, ldd,
+                                         _stream_on(ctx, stream))
+    if rc:
+        _check(rc, ctx.h)
 
 
 def peagle_adamw_step(ctx, tensors: AdamWTensors, lr, beta1, beta2, eps, step=1, seed=0, lr_dev=None, step_dev=None,
                       grad_scale=None, stream=None):
     """One AdamW step over ``tensors``, in place.  ``lr_dev`` (fp32), ``step_dev`` (int64) and ``grad_scale`` (fp32) are
-    one-element device tensors that replace lr, step and the gradients' factor 1."""
-    import torch
-    for t, dtype in ((lr_dev, torch.float32), (step_dev, torch.int64), (grad_scale, torch.float32)):
-        _require(t is None or (t.numel() == 1 and t.dtype == dtype))
-    _on(ctx, lr_dev, step_dev, grad_scale)
-    _require(tensors.device is None or tensors.device == ctx.device)
-    how = peagle_adamw_t(float(lr), float(beta1), float(beta2), float(eps), int(step), _ptr(lr_dev), _ptr(step_dev),
-                         _ptr(grad_scale), int(seed) & 0xFFFFFFFF)
-    _check(lib().peagle_adamw_step(ctx.h, ctypes.byref(how), tensors.c, len(tensors.items), _stream_on(ctx, stream)), ctx.h)
+    device tensors of shape [1] that replace lr, step and the gradients' factor 1."""
+    dev = ctx.device
+    if tensors.device is not None and tensors.device != dev:
+        _refuse()
+    how = peagle_adamw_t(lr, beta1, beta2, eps, step, _vector(lr_dev, 1, _f32, dev), _vector(step_dev, 1, _i64, dev),
+                         _vector(grad_scale, 1, _f32, dev), seed & 0xFFFFFFFF)
+    rc = lib().peagle_adamw_step(ctx.h, ctypes.addressof(how), ctypes.addressof(tensors.c), len(tensors.items),
+                                 _stream_on(ctx, stream))
+    if rc:
+        _check(rc, ctx.h)
 
 
 def peagle_selftest_wait_expiry(ctx, limit_ms: int = 20, stream=None):
