@@ -52,7 +52,6 @@ template <class T, bool VEC, int TPR, int E>
 struct Part {
     static constexpr int PIECE = VEC ? 16 / (int)sizeof(T) : 1;
     static constexpr int N = E / PIECE;
-    [[maybe_unused]] static constexpr int BT = block_threads(TPR);
     static constexpr bool PACKED = VEC && sizeof(T) == 2; // bf16 pairs stay packed
     static constexpr int WORDS = PACKED ? E / 2 : E;
     uint32_t raw[WORDS];
@@ -73,7 +72,7 @@ struct Part {
 #pragma unroll
             for (int n = 0; n < N; ++n)
                 if ((n * TPR + t) * PIECE < cols)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage + n * BT * 16),
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage + n * block_threads(TPR) * 16),
                                  "l"(row + n * TPR * PIECE)
                                  : "memory");
         }
@@ -85,7 +84,7 @@ struct Part {
 #pragma unroll
             for (int n = 0; n < N; ++n)
                 if ((n * TPR + t) * PIECE >= cols)
-                    stage[n * BT] = make_uint4(0, 0, 0, 0);
+                    stage[n * block_threads(TPR)] = make_uint4(0, 0, 0, 0);
         }
     }
     __device__ __forceinline__ void take(const T *row, int t, int cols, const uint4 *stage)
@@ -93,7 +92,7 @@ struct Part {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             if constexpr (VEC) {
-                const uint4 v = stage[n * BT];
+                const uint4 v = stage[n * block_threads(TPR)];
                 raw[4 * n] = v.x;
                 raw[4 * n + 1] = v.y;
                 raw[4 * n + 2] = v.z;
@@ -211,9 +210,9 @@ __device__ __forceinline__ float2 group_sum2(F2 v, float2 (*red)[block_threads(T
         asm volatile("bar.sync %0, %1;" ::"r"(1 + group), "n"(TPR) : "memory");
         v = f2(0.f, 0.f);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            const float2 u = red[turn][group * W + i];
-            v = add_f2(v, f2(u.x, u.y));
+        for (int i = 0; i < W; i += 2) {
+            const float4 u = *reinterpret_cast<const float4 *>(&red[turn][group * W + i]);
+            v = add_f2(add_f2(v, f2(u.x, u.y)), f2(u.z, u.w));
         }
         turn ^= 1;
     }
@@ -235,6 +234,19 @@ __device__ __forceinline__ void stage_weights(float *to, const void *w, int dtyp
     }
 }
 
+// The forward's blocks per SM.  RMS norm is best with 32 to 64 KB of rows on their way; more in flight is slower:
+// rows of 2,880 bf16 take 63.6 us with 768 threads and 70.9 with 1,152, of 2,880 fp32 64.8 with 512 and 70.0 with
+// 768, of 128 bf16 47.1 with 512 and 50.8 with 768; 8,192 bf16 in blocks of 512 threads 55.3 us with one and 47.3
+// with two.  Layer norm has two sums to wait for and takes all the threads that fit (2,880 fp32: 77 us with 512,
+// 67 with 768; 128 bf16 59 and 53).
+constexpr int fwd_blocks(bool layer, int words, int tpr, int threads)
+{
+    if (layer)
+        return 32;
+
+    const int want = words > 8 || tpr < 32 ? 512 : tpr == 512 ? 1024 : 768;
+    return want < threads ? 1 : want / threads;
+}
 template <class T, bool VEC, int TPR, int E>
 __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __grid_constant__ NormArgs a)
 {
@@ -245,33 +257,33 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
     uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
     float *sw = reinterpret_cast<float *>(smem + D * STAGE), *sb = sw + TPR * E;
     __shared__ float red1[2][BT / 32];
-    __shared__ float2 red2[2][BT / 32];
+    __shared__ __align__(16) float2 red2[2][BT / 32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
     const bool layer = a.kind == PEAGLE_NORM_LAYER;
     const uint32_t rows = a.rows, step = gridDim.x * G, first = blockIdx.x * G + g;
-    const T *x_at = static_cast<const T *>(a.X) + first * a.ldx + t * Row::PIECE; // the row at hand
-    T *y_at = static_cast<T *>(a.Y) + first * a.ldy + t * Row::PIECE;
-    const int64_t x_step = step * a.ldx, y_step = step * a.ldy;
+    // formed anew for every row: pointers that move along would take registers
+    const auto x_at = [&](uint32_t r) { return static_cast<const T *>(a.X) + t * Row::PIECE + r * a.ldx; };
+    const auto y_at = [&](uint32_t r) { return static_cast<T *>(a.Y) + t * Row::PIECE + r * a.ldy; };
     uint32_t ring_at = smem_u32(ring);
 #pragma unroll
     for (int i = 0; i < D; ++i) {
         Row::clear(t, cols, ring + i * STAGE);
         if (first + i * step < rows)
-            Row::fetch(x_at + i * x_step, t, cols, ring_at + i * STAGE * 16);
+            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * 16);
         copies_commit();
     }
     stage_weights<Row, E, G>(sw, a.weight, a.w_dtype, 1.f, t, g, cols);
     if (a.bias)
         stage_weights<Row, E, G>(sb, a.bias, a.w_dtype, 0.f, t, g, cols);
     __syncthreads();
-    const float n = (float)cols;
+    const float per_col = 1.f / (float)cols;
     int turn = 0, stage = 0;
     // groups of less than a warp stay together with their warp
-    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows; r += step, x_at += x_step, y_at += y_step) {
+    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows; r += step) {
         Row x;
         copies_wait<D - 1>();
         if (VEC || r < rows)
-            x.take(x_at, t, cols, ring + stage * STAGE);
+            x.take(x_at(r), t, cols, ring + stage * STAGE);
         float mu = 0.f, var;
         if (layer) {
             F2 s = f2(0.f, 0.f), q = s;
@@ -279,7 +291,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
             for (int e = 0; e < E; e += 2)
                 s = add_f2(s, x.get2(e));
             const float2 sum = unf2(s);
-            mu = group_sum<TPR>(sum.x + sum.y, red1, turn) / n;
+            mu = group_sum<TPR>(sum.x + sum.y, red1, turn) * per_col;
             const F2 minus = f2(-mu, -mu);
             s = q;
 #pragma unroll
@@ -296,20 +308,20 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
             }
             const float2 s2 = unf2(s), q2 = unf2(q);
             const float2 both = group_sum2<TPR>(f2(s2.x + s2.y, q2.x + q2.y), red2, turn);
-            const float left = both.x / n; // the rounding of mu is taken out of both
+            const float left = both.x * per_col; // the rounding of mu is taken out of both
             mu += left;
-            var = both.y / n - left * left;
+            var = both.y * per_col - left * left;
         } else {
             F2 q = f2(0.f, 0.f);
 #pragma unroll
             for (int e = 0; e < E; e += 2)
                 q = fma_f2(x.get2(e), x.get2(e), q);
             const float2 q2 = unf2(q);
-            var = group_sum<TPR>(q2.x + q2.y, red1, turn) / n;
+            var = group_sum<TPR>(q2.x + q2.y, red1, turn) * per_col;
         }
         // the sums are formed, so the stage has been read
         if (r + D * step < rows)
-            Row::fetch(x_at + D * x_step, t, cols, ring_at + stage * STAGE * 16);
+            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * 16);
         copies_commit();
         if (D > 1)
             stage ^= 1;
@@ -340,7 +352,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
             x.set2(e + 2, v1);
         }
         if (r < rows) {
-            x.store(y_at, t, cols);
+            x.store(y_at(r), t, cols);
             if (t == 0) {
                 if (a.mean)
                     a.mean[r] = mu;
@@ -351,8 +363,10 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
     }
 }
 
-// SUMS: 0 none, 1 of dy xh (dw), 2 of dy too (db).
-template <class T, bool VEC, int TPR, int E, int SUMS>
+// LAYER: layer norm, else RMS norm.  SUMS: 1 of dy xh (dw), 2 of dy too (db).  With z = x - mu the products are
+// arranged for few operations per element: t = dy z gives sum u xh = rstd sum t w and dw += rstd t, and
+// dx = rstd w dy + (-rstd^2 mean(u xh)) z - rstd mean(u).
+template <class T, bool VEC, bool LAYER, int TPR, int E, int SUMS>
 __global__ void __launch_bounds__(block_threads(TPR),
                                   blocks_per_sm(block_threads(TPR), 2 * Part<T, VEC, TPR, E>::WORDS + SUMS * E))
     norm_bwd_kernel(const __grid_constant__ NormArgs a)
@@ -363,55 +377,53 @@ __global__ void __launch_bounds__(block_threads(TPR),
     extern __shared__ float4 smem[];
     uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
     float *sw = reinterpret_cast<float *>(smem + D * STAGE);
-    __shared__ float2 red[2][BT / 32];
+    __shared__ float red1[2][BT / 32];
+    __shared__ __align__(16) float2 red[2][BT / 32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
-    const bool layer = a.kind == PEAGLE_NORM_LAYER;
     const uint32_t rows = a.rows, step = gridDim.x * G, first = blockIdx.x * G + g;
-    const T *x_at = static_cast<const T *>(a.X) + first * a.ldx + t * Row::PIECE;
-    const T *dy_at = static_cast<const T *>(a.dY) + first * a.lddy + t * Row::PIECE;
-    T *dx_at = static_cast<T *>(a.dX) + first * a.lddx + t * Row::PIECE;
-    const int64_t x_step = step * a.ldx, dy_step = step * a.lddy, dx_step = step * a.lddx;
+    // formed anew for every row, like the forward's
+    const auto x_at = [&](uint32_t r) { return static_cast<const T *>(a.X) + t * Row::PIECE + r * a.ldx; };
+    const auto dy_at = [&](uint32_t r) { return static_cast<const T *>(a.dY) + t * Row::PIECE + r * a.lddy; };
+    const auto dx_at = [&](uint32_t r) { return static_cast<T *>(a.dX) + t * Row::PIECE + r * a.lddx; };
     const uint32_t ring_at = smem_u32(ring);
 #pragma unroll
     for (int i = 0; i < D; ++i) {
         Row::clear(t, cols, ring + i * STAGE);
         Row::clear(t, cols, ring + i * STAGE + HALF);
         if (first + i * step < rows) {
-            Row::fetch(x_at + i * x_step, t, cols, ring_at + i * STAGE * 16);
-            Row::fetch(dy_at + i * dy_step, t, cols, ring_at + (i * STAGE + HALF) * 16);
+            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * 16);
+            Row::fetch(dy_at(first + i * step), t, cols, ring_at + (i * STAGE + HALF) * 16);
         }
         copies_commit();
     }
     float mu = 0.f, rstd = 0.f; // of the row to come
     if (first < rows) {
-        mu = layer ? a.mean_in[first] : 0.f;
+        mu = LAYER ? a.mean_in[first] : 0.f;
         rstd = a.rstd_in[first];
     }
     stage_weights<Row, E, G>(sw, a.weight, a.w_dtype, 1.f, t, g, cols);
     __syncthreads();
-    F2 dw[SUMS > 0 ? E / 2 : 1], db[SUMS > 1 ? E / 2 : 1];
+    F2 dw[E / 2], db[SUMS > 1 ? E / 2 : 1];
 #pragma unroll
     for (int e = 0; e < E / 2; ++e) {
-        if (SUMS > 0)
-            dw[e] = f2(0.f, 0.f);
+        dw[e] = f2(0.f, 0.f);
         if (SUMS > 1)
             db[e] = f2(0.f, 0.f);
     }
-    const float n = (float)cols;
+    const float per_col = 1.f / (float)cols;
     int turn = 0, stage = 0;
-    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows;
-         r += step, x_at += x_step, dy_at += dy_step, dx_at += dx_step) {
+    for (uint32_t r = first; r - (TPR < 32 ? g % (32 / TPR) : 0) < rows; r += step) {
         Row x, dy;
         const F2 minus = f2(-mu, -mu), by = f2(rstd, rstd);
         const float rs = rstd;
         if (r + step < rows) {
-            mu = layer ? a.mean_in[r + step] : 0.f;
+            mu = LAYER ? a.mean_in[r + step] : 0.f;
             rstd = a.rstd_in[r + step];
         }
         copies_wait<D - 1>();
         if (VEC || r < rows) {
-            x.take(x_at, t, cols, ring + stage * STAGE);
-            dy.take(dy_at, t, cols, ring + stage * STAGE + HALF);
+            x.take(x_at(r), t, cols, ring + stage * STAGE);
+            dy.take(dy_at(r), t, cols, ring + stage * STAGE + HALF);
         }
         if (TPR < 32 && r >= rows) {
             x.zero();
@@ -424,26 +436,30 @@ __global__ void __launch_bounds__(block_threads(TPR),
             Row::weights4(sw, t, e, w[0], w[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const F2 d = dy.get2(e + 2 * k), xh = mul_f2(add_f2(x.get2(e + 2 * k), minus), by), u = mul_f2(d, w[k]);
-                s0 = add_f2(s0, u);
-                s1 = fma_f2(u, xh, s1);
-                if (SUMS > 0)
-                    dw[e / 2 + k] = fma_f2(d, xh, dw[e / 2 + k]);
+                const F2 d = dy.get2(e + 2 * k), x2 = x.get2(e + 2 * k), td = mul_f2(d, LAYER ? add_f2(x2, minus) : x2);
+                if (LAYER)
+                    s0 = fma_f2(d, w[k], s0);
+                s1 = fma_f2(td, w[k], s1);
+                dw[e / 2 + k] = fma_f2(td, by, dw[e / 2 + k]);
                 if (SUMS > 1)
                     db[e / 2 + k] = add_f2(db[e / 2 + k], d);
             }
         }
         const float2 p0 = unf2(s0), p1 = unf2(s1);
-        const float2 s = group_sum2<TPR>(f2(p0.x + p0.y, p1.x + p1.y), red, turn);
+        float2 s;
+        if (LAYER)
+            s = group_sum2<TPR>(f2(p0.x + p0.y, p1.x + p1.y), red, turn);
+        else
+            s = make_float2(0.f, group_sum<TPR>(p1.x + p1.y, red1, turn));
         // the sums are formed, so the stage has been read
         if (r + D * step < rows) {
-            Row::fetch(x_at + D * x_step, t, cols, ring_at + stage * STAGE * 16);
-            Row::fetch(dy_at + D * dy_step, t, cols, ring_at + (stage * STAGE + HALF) * 16);
+            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * 16);
+            Row::fetch(dy_at(r + D * step), t, cols, ring_at + (stage * STAGE + HALF) * 16);
         }
         copies_commit();
         if (D > 1)
             stage ^= 1;
-        const float c0 = layer ? -rs * (s.x / n) : 0.f, c1 = -rs * (s.y / n);
+        const float c0 = -rs * per_col * s.x, c1 = -rs * rs * rs * per_col * s.y;
         x.forget();
         dy.forget();
 #pragma unroll
@@ -452,52 +468,53 @@ __global__ void __launch_bounds__(block_threads(TPR),
             Row::weights4(sw, t, e, w[0], w[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const F2 u = mul_f2(dy.get2(e + 2 * k), w[k]), xh = mul_f2(add_f2(x.get2(e + 2 * k), minus), by);
-                x.set2(e + 2 * k, fma_f2(xh, f2(c1, c1), fma_f2(u, by, f2(c0, c0))));
+                const F2 x2 = x.get2(e + 2 * k);
+                const F2 rest = LAYER ? fma_f2(add_f2(x2, minus), f2(c1, c1), f2(c0, c0)) : mul_f2(x2, f2(c1, c1));
+                x.set2(e + 2 * k, fma_f2(dy.get2(e + 2 * k), mul_f2(w[k], by), rest));
             }
         }
         if (r < rows)
-            x.store(dx_at, t, cols);
+            x.store(dx_at(r), t, cols);
     }
     copies_wait<0>();
     pdl_trigger(); // the kernel that joins the blocks may settle down
-    if constexpr (SUMS > 0) {
+    if (!a.dw && !a.db)
+        return;
 #pragma unroll
-        for (int which = 0; which < SUMS; ++which) {
-            float *out = which ? a.db : a.dw;
-            float *part = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * cols;
-            const auto mine = [&](int e) {
-                const float2 v = unf2(which ? db[SUMS > 1 ? e / 2 : 0] : dw[e / 2]);
-                return e & 1 ? v.y : v.x;
-            };
-            const auto leave = [&](int c, float v) {
-                if (gridDim.x > 1)
-                    part[c] = v;
-                else if (out)
-                    out[c] += v;
-            };
-            if (G == 1) {
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (Row::col(t, e) < cols)
-                        leave(Row::col(t, e), mine(e));
-                continue;
-            }
-            __syncthreads(); // weights, and the sums before, have been read
+    for (int which = 0; which < SUMS; ++which) {
+        float *out = which ? a.db : a.dw;
+        float *part = a.partial + ((size_t)which * gridDim.x + blockIdx.x) * cols;
+        const auto mine = [&](int e) {
+            const float2 v = unf2(which ? db[SUMS > 1 ? e / 2 : 0] : dw[e / 2]);
+            return e & 1 ? v.y : v.x;
+        };
+        const auto leave = [&](int c, float v) {
+            if (gridDim.x > 1)
+                part[c] = v;
+            else if (out)
+                out[c] += v;
+        };
+        if (G == 1) {
 #pragma unroll
             for (int e = 0; e < E; ++e)
-                sw[(g * E + e) * TPR + t] = mine(e);
-            __syncthreads();
-            for (int i = threadIdx.x; i < TPR * E; i += BT) {
-                const int c = Row::col(i % TPR, i / TPR);
-                if (c >= cols)
-                    continue;
-                float v = 0.f;
+                if (Row::col(t, e) < cols)
+                    leave(Row::col(t, e), mine(e));
+            continue;
+        }
+        __syncthreads(); // weights, and the sums before, have been read
 #pragma unroll
-                for (int k = 0; k < G; ++k)
-                    v += sw[k * E * TPR + i];
-                leave(c, v);
-            }
+        for (int e = 0; e < E; ++e)
+            sw[(g * E + e) * TPR + t] = mine(e);
+        __syncthreads();
+        for (int i = threadIdx.x; i < TPR * E; i += BT) {
+            const int c = Row::col(i % TPR, i / TPR);
+            if (c >= cols)
+                continue;
+            float v = 0.f;
+#pragma unroll
+            for (int k = 0; k < G; ++k)
+                v += sw[k * E * TPR + i];
+            leave(c, v);
         }
     }
 }
@@ -652,10 +669,10 @@ int with_group(int cols, bool vec, F f)
     if (vec) {
         if (cols <= 8 * 8)
             return f.template operator()<T, true, 8, 8>();
-        if (cols <= 16 * 8)
-            return f.template operator()<T, true, 16, 8>();
-        if (cols <= 32 * 8)
-            return f.template operator()<T, true, 32, 8>();
+        if (cols <= 8 * 16)
+            return f.template operator()<T, true, 8, 16>();
+        if (cols <= 16 * 16)
+            return f.template operator()<T, true, 16, 16>();
         if (cols <= 32 * 16)
             return f.template operator()<T, true, 32, 16>();
         if (cols <= 64 * 16)
@@ -681,9 +698,10 @@ int with_group(int cols, bool vec, F f)
     return f.template operator()<T, false, 1024, 16>();
 }
 
-// Blocks of `kernel` that fit the GPU at once, at most one for every `per_block` rows.  `known` keeps how many
+// Blocks of `kernel` that fit the GPU at once, at most `most` to an SM and one for every `per_block` rows.  `known` keeps how many
 // fit an SM (all devices here are alike; asking takes longer than a short row).
-int blocks_for(const void *kernel, int threads, size_t smem, std::atomic<int> &known, int n_sm, int64_t rows, int per_block)
+int blocks_for(const void *kernel, int threads, size_t smem, std::atomic<int> &known, int most, int n_sm, int64_t rows,
+               int per_block)
 {
     if (smem > 40 * 1024) // the kernels' own arrays count towards the 48 KB too
         cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -693,6 +711,7 @@ int blocks_for(const void *kernel, int threads, size_t smem, std::atomic<int> &k
             cudaGetLastError();
             per_sm = 1;
         }
+        per_sm = std::min(per_sm, most);
         known.store(per_sm, std::memory_order_relaxed);
     }
     return (int)std::min<int64_t>((rows + per_block - 1) / per_block, (int64_t)n_sm * per_sm);
@@ -707,10 +726,12 @@ struct Forward {
     {
         constexpr int BT = block_threads(TPR);
         const auto kernel = norm_fwd_kernel<T, VEC, TPR, E>;
-        static std::atomic<int> known[2];
+        static std::atomic<int> known[4];
         const size_t smem = (size_t)Ring<T, VEC, TPR, E, 1>::BYTES * BT + (size_t)(a.bias ? 2 : 1) * TPR * E * sizeof(float);
-        kernel<<<blocks_for((const void *)kernel, BT, smem, known[a.bias != nullptr], n_sm, a.rows, BT / TPR), BT, smem,
-                 s>>>(a);
+        const bool layer = a.kind == PEAGLE_NORM_LAYER;
+        const int blocks = blocks_for((const void *)kernel, BT, smem, known[2 * layer + (a.bias != nullptr)],
+                                      fwd_blocks(layer, Part<T, VEC, TPR, E>::WORDS, TPR, BT), n_sm, a.rows, BT / TPR);
+        kernel<<<blocks, BT, smem, s>>>(a);
         return 1;
     }
 };
@@ -723,25 +744,23 @@ struct Backward {
     template <class T, bool VEC, int TPR, int E>
     int operator()() const
     {
-        if (a.db)
-            return with_sums<T, VEC, TPR, E, 2>();
-        if (a.dw)
-            return with_sums<T, VEC, TPR, E, 1>();
-        return with_sums<T, VEC, TPR, E, 0>();
+        if (a.kind == PEAGLE_NORM_LAYER)
+            return a.db ? with_sums<T, VEC, true, TPR, E, 2>() : with_sums<T, VEC, true, TPR, E, 1>();
+        return a.db ? with_sums<T, VEC, false, TPR, E, 2>() : with_sums<T, VEC, false, TPR, E, 1>();
     }
-    template <class T, bool VEC, int TPR, int E, int SUMS>
+    template <class T, bool VEC, bool LAYER, int TPR, int E, int SUMS>
     int with_sums() const
     {
         constexpr int BT = block_threads(TPR);
-        const auto kernel = norm_bwd_kernel<T, VEC, TPR, E, SUMS>;
+        const auto kernel = norm_bwd_kernel<T, VEC, LAYER, TPR, E, SUMS>;
         // the rows to come; weights, then the sums of the block's groups
-        const size_t smem = (size_t)Ring<T, VEC, TPR, E, 2>::BYTES * BT + (size_t)(SUMS > 0 ? BT : TPR) * E * sizeof(float);
+        const size_t smem = (size_t)Ring<T, VEC, TPR, E, 2>::BYTES * BT + (size_t)BT * E * sizeof(float);
         static std::atomic<int> known;
-        const int blocks = blocks_for((const void *)kernel, BT, smem, known, n_sm, a.rows, BT / TPR);
+        const int blocks = blocks_for((const void *)kernel, BT, smem, known, 32, n_sm, a.rows, BT / TPR);
         if (only_blocks)
             return blocks;
         kernel<<<blocks, BT, smem, s>>>(a);
-        if (SUMS == 0 || blocks == 1)
+        if ((!a.dw && !a.db) || blocks == 1)
             return 1;
         cudaLaunchConfig_t cfg = {};
         cudaLaunchAttribute at[1];
