@@ -351,7 +351,7 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
  * 0) and top_logprobs = s_id - lse.  logits is dev [rows][vocab] of `dtype`; tokens dev int32 [rows], -1
  * where a row has no token: its logprob is 0, all else as for any row.  logprob, lse, entropy are dev fp32
  * [rows], top_logprobs fp32 and top_ids int32 [rows][top_k] (contiguous); each may be NULL, tokens too when
- * logprob is.  0 <= top_k <= min(vocab, PEAGLE_MAX_TOP_K), and the two top outputs are either both there or
+ * logprob is.  vocab <= 2^30, 0 <= top_k <= min(vocab, PEAGLE_MAX_TOP_K), and the two top outputs are either both there or
  * both NULL (top_k == 0).  -inf is a token of probability zero, and
  *   - a row of nothing but -inf (or logits that scale takes there) has lse = logprob = -inf, entropy 0, top
  *     ids 0, 1, .. with log probability -inf;

@@ -1358,7 +1358,7 @@ static int logprob_args_ok(int32_t dtype, int32_t rows, int32_t vocab, int64_t l
 {
     if (!dtype_size(dtype) || rows < 0 || vocab < 1 || ld < vocab || !(scale > 0.f && scale <= 1e20f))
         return PEAGLE_ERR_BAD_SHAPE;
-    return PEAGLE_OK;
+    return vocab > 1 << 30 ? PEAGLE_ERR_TOO_LARGE : PEAGLE_OK;
 }
 
 int peagle_token_logprobs_fwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
@@ -1439,7 +1439,10 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
     a.ldd = ldd;
     const OnDevice on(ctx->device);
     CK(on.error);
-    ctx->launches += launch_logprobs_bwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    const int n = launch_logprobs_bwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    if (n < 0)
+        return n;
+    ctx->launches += n;
     CK(cudaGetLastError());
     return PEAGLE_OK;
 }

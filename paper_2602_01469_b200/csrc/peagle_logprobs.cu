@@ -1,11 +1,24 @@
 // Log probabilities of given tokens, entropy and top alternatives of rows of logits, and the gradient.
 //
-// With m the row's maximum, t_j = scale (x_j - m), S = sum exp(t_j), E = sum exp(t_j) t_j:
-//     lse = scale m + log S,   logprob = t_token - log S,   entropy = log S - E / S
-// (the differences to m are formed first, so that logprob and entropy do not lose the digits that a large
-// m would take).  Backward, with log p = scale x - lse:
+// Forward: one read of the logits.  In powers of two, with l = scale log2(e), m the maximum and c = m l rounded:
+//     t_j = x_j l - c,  S = sum 2^t_j,  E = sum 2^t_j t_j,  log S = ln 2 (log2 S - (m l - c))
+//     lse = scale m + log S,  logprob = scale (x_token - m) - log S,  entropy = ln 2 (log2 S - E / S)
+// where x l - c and m l - c are fused operations: logprob and entropy do not lose the digits that a large m would
+// take.  A thread keeps (m, S, E) and rescales them when its maximum grows; threads, then blocks, join theirs.
+// Backward, with log p = scale x - lse:
 //     dx_j = scale ( g ([j = token] - p_j) - h p_j (log p_j + entropy) ).
+//
+// Bound by memory.  A block takes a row in chunks of 16 bytes per thread and load, the next chunk on its way.  Few
+// rows are cut into parts for a cluster of up to 8 blocks, which join through distributed shared memory.
+//
+// Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
+// k-th largest of the threads' maxima, then the k-th best entry so far).  A chunk's maximum, which the sums need
+// anyway, says whether it holds anything to add; what reaches the bound goes to a list in shared memory, with room
+// for a whole chunk, and a long list is cut to its k best.  Entries are compared by value, then by id, so the result
+// does not depend on the order in which they came.
 #include <cuda_bf16.h>
+
+#include <algorithm>
 
 #include "peagle_internal.h"
 #include "sm100_ptx.cuh"
@@ -15,12 +28,18 @@ using namespace sm100;
 
 namespace {
 
-constexpr int LP_THREADS = 256;
+constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
+constexpr int CHUNK = 4096;      // entries per chunk
+constexpr int LONG_LIST = 256;   // a list longer than this is cut down between chunks
+constexpr int COUNTED = 2 * LP_THREADS; // entries that are ranked by counting, at most
+constexpr int MAX_CLUSTER = 8;
+static_assert(MAX_CLUSTER * PEAGLE_MAX_TOP_K <= COUNTED, "the lists of a cluster are ranked at once");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float T_FLOOR = -300.f; // below this, in powers of two, a probability is zero in fp32
 constexpr float LSE_LARGE = 8192.f; // from here on fp32 keeps less than 2^-10 of a log-sum-exp
-constexpr float NEG_INF = -__builtin_huge_valf();
+constexpr float INF = __builtin_huge_valf();
 
+__device__ __forceinline__ float nan_f32() { return __int_as_float(0x7fffffff); }
 __device__ __forceinline__ float to_f32(float v) { return v; }
 __device__ __forceinline__ float to_f32(__nv_bfloat16 v) { return __bfloat162float(v); }
 __device__ __forceinline__ void from_f32(float *p, float v) { *p = v; }
@@ -34,13 +53,13 @@ __device__ __forceinline__ uint32_t order_key(float x)
 }
 __device__ __forceinline__ float from_key(uint32_t k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 
-// Larger value first, then the lower id.
+// Larger value first, then the lower id.  0: no entry.
 __device__ __forceinline__ uint64_t rank_key(float x, int id) { return (uint64_t)order_key(x) << 32 | (uint32_t)~id; }
 
 template <class V, class F>
 __device__ __forceinline__ V block_join(V v, F f)
 {
-    __shared__ V part[LP_THREADS / 32];
+    __shared__ V part[LP_WARPS];
     for (int o = 16; o; o >>= 1)
         v = f(v, __shfl_xor_sync(~0u, v, o));
     __syncthreads();
@@ -48,143 +67,528 @@ __device__ __forceinline__ V block_join(V v, F f)
         part[threadIdx.x >> 5] = v;
     __syncthreads();
     v = part[0];
-    for (int i = 1; i < LP_THREADS / 32; ++i)
+    for (int i = 1; i < LP_WARPS; ++i)
         v = f(v, part[i]);
     return v;
 }
 
-// Writes a row's outputs but the top alternatives; log S as it returns is what they need.
-__device__ __forceinline__ float write_row(const LogprobArgs &a, int r, float m, float S, float E, float x_token, int token)
+// ------------------------------------------------------------------ sums
+
+struct Sums {
+    float m, S, E; // E in powers of two
+};
+
+// What S and E refer to.  Without a maximum S is 0 (or NaN), whatever they refer to.  The bounds keep it a number
+// where m l is none, so that rescaling such a sum by 2^-huge leaves 0 and not NaN.
+__device__ __forceinline__ float reference(float m, float l)
 {
-    const float ms = m * a.scale;
-    float lse, logS = logf(S), H = logS - E * LN2 / S, lp = (x_token - m) * a.scale - logS;
-    lse = ms + logS;
-    if (ms == -NEG_INF || !(S == S))
-        lse = H = lp = logS = __int_as_float(0x7fffffff);
-    else if (ms == NEG_INF) {
-        lse = lp = NEG_INF;
-        H = 0.f;
+    return m == -INF ? 0.f : fminf(fmaxf(m * l, -3.4028235e38f), 3.4028235e38f);
+}
+
+__device__ __forceinline__ void rescale(Sums &s, float m, float l)
+{
+    if (s.m != -INF && s.m != m) {
+        const float d = reference(s.m, l) - reference(m, l), f = exp2f(d);
+        s.E = f * fmaf(s.S, fmaxf(d, T_FLOOR), s.E);
+        s.S *= f;
     }
+    s.m = m;
+}
+
+__device__ __forceinline__ Sums join(Sums a, Sums b, float l)
+{
+    const float m = fmaxf(a.m, b.m);
+    rescale(a, m, l);
+    rescale(b, m, l);
+    return {m, a.S + b.S, a.E + b.E};
+}
+
+// What a row's log probabilities are formed with: scale (x - m) - logS.
+struct RowStats {
+    float m, logS, H;
+    bool none, empty; // NaN or +inf in the row; nothing but -inf
+};
+
+// `c`: what S and E refer to, m l but for the rounding.
+__device__ __forceinline__ RowStats row_stats(Sums s, float c, float scale)
+{
+    RowStats w;
+    const float log2S = log2f(s.S);
+    w.m = s.m;
+    w.logS = (log2S - (c == 0.f ? 0.f : fmaf(s.m, scale * LOG2E, -c))) * LN2;
+    w.H = (log2S - s.E / s.S) * LN2;
+    w.empty = s.S == 0.f || s.m * scale == -INF; // S of a row with a maximum is about 1 or more
+    w.none = s.S != s.S || s.m * scale == INF;
+    return w;
+}
+
+__device__ __forceinline__ float logprob_of(const RowStats &w, float x, float scale)
+{
+    return w.none ? nan_f32() : w.empty ? -INF : fmaf(x - w.m, scale, -w.logS);
+}
+
+__device__ __forceinline__ void write_row(const LogprobArgs &a, int r, const RowStats &w, float x_token, int token)
+{
+    float lp = logprob_of(w, x_token, a.scale);
     if (token == -1)
         lp = 0.f;
     else if (token < 0 || token >= a.vocab) {
-        lp = __int_as_float(0x7fffffff);
+        lp = nan_f32();
         if (a.logprob)
             atomicCAS(a.status, 0, PEAGLE_ERR_BAD_META);
     }
     if (a.logprob)
         a.logprob[r] = lp;
     if (a.lse)
-        a.lse[r] = lse;
+        a.lse[r] = w.none ? nan_f32() : w.empty ? -INF : fmaf(w.m, a.scale, w.logS);
     if (a.entropy)
-        a.entropy[r] = H;
-    return logS;
+        a.entropy[r] = w.none ? nan_f32() : w.empty ? 0.f : w.H;
 }
 
-// One of the top alternatives of a row: its place in the order, its logit and id.
-__device__ __forceinline__ void write_top(const LogprobArgs &a, int r, int place, uint64_t key, float m, float logS)
-{
-    const float x = from_key((uint32_t)(key >> 32));
-    const bool none = logS != logS, empty = m * a.scale == NEG_INF;
-    a.top[(size_t)r * a.top_k + place] = none ? logS : empty ? NEG_INF : (x - m) * a.scale - logS;
-    a.ids[(size_t)r * a.top_k + place] = none ? -1 : (int)~(uint32_t)key;
-}
+// ------------------------------------------------------------------ lists of the best entries
 
-template <class T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_fwd_rows(const LogprobArgs a)
+// Sorts a list and cuts it to its k best.  The whole block; a barrier before and after.  Returns the new length.
+__device__ __forceinline__ int cut_list(uint64_t *list, int n, int k)
 {
-    const int r = blockIdx.x;
-    const T *x = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-    float m = NEG_INF;
-    for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
-        m = fmaxf(m, to_f32(x[j]));
-    m = block_join(m, [](float p, float q) { return fmaxf(p, q); });
-    const float from = m == NEG_INF ? 0.f : m, sl = a.scale * LOG2E;
-    float S = 0.f, E = 0.f;
-    for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
-        const float t = (to_f32(x[j]) - from) * sl, e = exp2f(t);
-        S += e;
-        E = fmaf(e, fmaxf(t, T_FLOOR), E);
-    }
-    S = block_join(S, [](float p, float q) { return p + q; });
-    E = block_join(E, [](float p, float q) { return p + q; });
-    const int token = a.tokens ? a.tokens[r] : -1;
-    float logS = 0.f;
-    __shared__ float shared_logS;
-    if (threadIdx.x == 0)
-        shared_logS = write_row(a, r, m, S, E, token >= 0 && token < a.vocab ? to_f32(x[token]) : 0.f, token);
-    __syncthreads();
-    logS = shared_logS;
-    uint64_t last = ~0ull;
-    for (int i = 0; i < a.top_k; ++i) {
-        uint64_t best = 0;
-        for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
-            const uint64_t k = rank_key(to_f32(x[j]), j);
-            if (k < last && k > best)
-                best = k;
+    __shared__ uint64_t kept[PEAGLE_MAX_TOP_K];
+    __shared__ int kept_n;
+    if (n > COUNTED) { // the k-th best entry bit by bit, then what is not below it
+        uint64_t bound = 0;
+        for (int bit = 63; bit >= 0; --bit) {
+            const uint64_t trial = bound | 1ull << bit;
+            int c = 0;
+            for (int i = threadIdx.x; i < n; i += LP_THREADS)
+                c += list[i] >= trial;
+            if (block_join(c, [](int p, int q) { return p + q; }) >= k)
+                bound = trial;
         }
-        last = block_join(best, [](uint64_t p, uint64_t q) { return p > q ? p : q; });
         if (threadIdx.x == 0)
-            write_top(a, r, i, last, m, logS);
+            kept_n = 0;
+        __syncthreads();
+        for (int i = threadIdx.x; i < n; i += LP_THREADS)
+            if (list[i] >= bound)
+                kept[atomicAdd(&kept_n, 1)] = list[i];
+        __syncthreads();
+        n = k;
+        if (threadIdx.x < k)
+            list[threadIdx.x] = kept[threadIdx.x];
+        __syncthreads();
+    }
+    // an entry's place is the number of better ones
+    uint64_t mine[2];
+    int place[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int i = threadIdx.x + j * LP_THREADS;
+        mine[j] = i < n ? list[i] : 0;
+        if (mine[j])
+            for (int o = 0; o < n; ++o)
+                place[j] += list[o] > mine[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+        if (mine[j] && place[j] < k)
+            list[place[j]] = mine[j];
+    __syncthreads();
+    return min(n, k);
+}
+
+__device__ __forceinline__ uint64_t load_remote(const uint64_t *p, uint32_t rank)
+{
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(cluster_map(smem_u32(p), rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ float load_remote(const float *p, uint32_t rank)
+{
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_map(smem_u32(p), rank)) : "memory");
+    return v;
+}
+
+// ------------------------------------------------------------------ forward
+
+// 16 bytes of a row: logits in order.
+template <class T>
+struct Piece {
+    static constexpr int N = 16 / sizeof(T);
+    uint4 v;
+    __device__ __forceinline__ void load(const T *p)
+    {
+        asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+            : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+            : "l"(p));
+    }
+    __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+    __device__ __forceinline__ float get(int e) const
+    {
+        if constexpr (sizeof(T) == 4)
+            return __uint_as_float(word(e));
+        else
+            return __uint_as_float(e & 1 ? word(e / 2) & 0xffff0000u : word(e / 2) << 16);
+    }
+    // Entries outside [lo, hi) become -inf.
+    __device__ __forceinline__ void mask(int lo, int hi)
+    {
+        uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (e < lo || e >= hi) {
+                if constexpr (sizeof(T) == 4)
+                    w[e] = 0xff800000u;
+                else
+                    w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | 0xff800000u : (w[e / 2] & 0xffff0000u) | 0xff80u;
+            }
+        v = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+__device__ __forceinline__ float piece_max(const Piece<float> &p, float m)
+{
+    return max3(max3(m, p.get(0), p.get(1)), p.get(2), p.get(3));
+}
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t r;
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ float piece_max(const Piece<__nv_bfloat16> &p, float m)
+{
+    const uint32_t w = max_bf16x2(max_bf16x2(p.v.x, p.v.y), max_bf16x2(p.v.z, p.v.w));
+    return max3(m, __uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+// A block per part of a row; `parts` blocks, a cluster, have a row.  part_len is a multiple of 8.
+template <class T, bool ENTROPY, bool TOP>
+__global__ void __launch_bounds__(LP_THREADS, 4)
+    logprobs_fwd_kernel(const __grid_constant__ LogprobArgs a, int parts, int part_len)
+{
+    constexpr int N = Piece<T>::N, U = CHUNK / (LP_THREADS * N);
+    extern __shared__ uint64_t list[]; // TOP: CHUNK + LONG_LIST entries
+    __shared__ int count;
+    __shared__ float4 first_max[LP_THREADS / 4];
+    __shared__ float first_bound;
+    __shared__ Sums warp_sums[LP_WARPS], sums;
+    __shared__ RowStats stats;
+    const int r = blockIdx.x / parts, part = blockIdx.x - r * parts;
+    const int begin = part * part_len, n = max(0, min(a.vocab - begin, part_len));
+    const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
+    // whole 16-byte pieces that hold an entry of this part; `before` entries of the first belong elsewhere
+    const int before = (int)(reinterpret_cast<uintptr_t>(row + begin) % 16 / sizeof(T));
+    const T *x = row + begin - before;
+    const int pieces = n ? (before + n + N - 1) / N : 0;
+    const float l = a.scale * LOG2E;
+    const int token = a.tokens && part == 0 ? a.tokens[r] : -1;
+
+    const auto load = [&](Piece<T> (&p)[U], int first) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int i = first + u * LP_THREADS + threadIdx.x;
+            if (i < pieces)
+                p[u].load(x + (size_t)i * N);
+            if (i == 0 || i >= pieces - 1)
+                p[u].mask(i < pieces ? before - i * N : N, before + n - i * N);
+        }
+    };
+    Piece<T> now[U], next[U];
+    load(now, 0);
+    if (TOP && threadIdx.x == 0)
+        count = 0;
+    Sums s = {-INF, 0.f, 0.f};
+    float bound = -INF;  // an entry at or above it may be among the k best
+    for (int first = 0; first < pieces; first += U * LP_THREADS) {
+        if (first + U * LP_THREADS < pieces)
+            load(next, first + U * LP_THREADS);
+        float top = -INF;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            top = piece_max(now[u], top);
+        if (top > s.m)
+            rescale(s, top, l);
+        const float c = reference(s.m, l);
+        const F2 l2 = f2(l, l), minus = f2(-c, -c);
+        F2 S2 = f2(s.S, 0.f), E2 = f2(s.E, 0.f);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const F2 t = fma_f2(f2(now[u].get(e), now[u].get(e + 1)), l2, minus);
+                const float2 tv = unf2(t);
+                const F2 p = f2(fast_exp2(tv.x), fast_exp2(tv.y));
+                S2 = add_f2(S2, p);
+                if (ENTROPY)
+                    E2 = fma_f2(p, f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR)), E2);
+            }
+        const float2 Sv = unf2(S2), Ev = unf2(E2);
+        s.S = Sv.x + Sv.y;
+        s.E = Ev.x + Ev.y;
+        if (TOP) {
+            if (first == 0) { // the k-th largest of the threads' maxima
+                reinterpret_cast<float *>(first_max)[threadIdx.x] = top;
+                __syncthreads();
+                int above = 0, equal = 0;
+#pragma unroll 8
+                for (int i = 0; i < LP_THREADS / 4; ++i) {
+                    const float4 o = first_max[i];
+                    above += (o.x > top) + (o.y > top) + (o.z > top) + (o.w > top);
+                    equal += (o.x == top) + (o.y == top) + (o.z == top) + (o.w == top);
+                }
+                if (above < a.top_k && above + equal >= a.top_k)
+                    first_bound = top;
+                __syncthreads();
+                bound = first_bound;
+            }
+            int end = 0;
+            if (top >= bound) {
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float v = now[u].get(e);
+                        const int id = (first + u * LP_THREADS + threadIdx.x) * N + e - before;
+                        if (v >= bound && id >= 0 && id < n) {
+                            end = atomicAdd(&count, 1);
+                            list[end++] = rank_key(v, begin + id);
+                        }
+                    }
+            }
+            if (first == 0)
+                bound = from_key(order_key(bound) + 1); // k entries with lower ids reach it
+            if (__syncthreads_or(end > LONG_LIST)) {
+                cut_list(list, count, a.top_k);
+                if (threadIdx.x == 0)
+                    count = a.top_k;
+                bound = from_key((uint32_t)(list[a.top_k - 1] >> 32) + 1);
+                __syncthreads();
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            now[u] = next[u];
+    }
+
+    // join the threads' sums, then the blocks'
+    for (int o = 16; o; o >>= 1) {
+        const Sums other = {__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.S, o), __shfl_xor_sync(~0u, s.E, o)};
+        s = join(s, other, l);
+    }
+    if ((threadIdx.x & 31) == 0)
+        warp_sums[threadIdx.x >> 5] = s;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        s = warp_sums[0];
+        for (int i = 1; i < LP_WARPS; ++i)
+            s = join(s, warp_sums[i], l);
+        sums = s;
+    }
+    int have = 0;
+    if (TOP)
+        have = cut_list(list, count, a.top_k);
+    if (parts > 1) {
+        if (TOP && threadIdx.x >= have && threadIdx.x < a.top_k)
+            list[threadIdx.x] = 0;
+        cluster_sync_all();
+        if (part == 0) {
+            if (threadIdx.x == 0)
+                for (int p = 1; p < parts; ++p)
+                    s = join(s, {load_remote(&sums.m, p), load_remote(&sums.S, p), load_remote(&sums.E, p)}, l);
+            if (TOP) {
+                uint64_t theirs[MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS];
+#pragma unroll
+                for (int j = 0; j < MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS; ++j) {
+                    const int i = threadIdx.x + j * LP_THREADS;
+                    theirs[j] = i < parts * a.top_k ? load_remote(&list[i % a.top_k], i / a.top_k) : 0;
+                }
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS; ++j)
+                    list[threadIdx.x + j * LP_THREADS] = theirs[j];
+                __syncthreads();
+                have = cut_list(list, parts * a.top_k, a.top_k);
+            }
+        }
+        cluster_sync_all(); // nobody leaves while its lists are read
+        if (part != 0)
+            return;
+    }
+    const float x_token = token >= 0 && token < a.vocab ? to_f32(row[token]) : 0.f;
+    if (threadIdx.x == 0) {
+        sums = s;
+        stats = row_stats(s, reference(s.m, l), a.scale);
+        write_row(a, r, stats, x_token, token);
+    }
+    __syncthreads();
+    s = sums;
+    if (fabsf(s.m) < INF && fabsf(s.m * l) == INF) {
+        // m is a number and m l is not (a row of the type's lowest): again, with x - m in the place of x
+        const float m = s.m;
+        float S = 0.f, E = 0.f;
+        for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
+            const float t = (to_f32(row[j]) - m) * l, p = fast_exp2(t);
+            S += p;
+            E = fmaf(p, fmaxf(t, T_FLOOR), E);
+        }
+        S = block_join(S, [](float p, float q) { return p + q; });
+        E = block_join(E, [](float p, float q) { return p + q; });
+        if (threadIdx.x == 0) {
+            stats = row_stats({m, S, E}, 0.f, a.scale);
+            write_row(a, r, stats, x_token, token);
+        }
+        __syncthreads();
+    }
+    if (TOP && threadIdx.x < a.top_k) {
+        const RowStats w = stats;
+        const uint64_t key = list[threadIdx.x];
+        const size_t at = (size_t)r * a.top_k + threadIdx.x;
+        a.top[at] = logprob_of(w, from_key((uint32_t)(key >> 32)), a.scale);
+        a.ids[at] = w.none ? -1 : (int)~(uint32_t)key;
     }
 }
 
+// ------------------------------------------------------------------ backward
+
+constexpr int BWD_PIECES = 4; // 16-byte pieces per thread
+
+// A block per BWD_PIECES * LP_THREADS pieces of a row.
 template <class T>
-__global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_rows(const LogprobArgs a)
+__global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_constant__ LogprobArgs a, int parts)
 {
-    const int r = blockIdx.x;
-    const T *x = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
-    T *d = static_cast<T *>(a.dlogits) + (size_t)r * a.ldd;
+    constexpr int N = Piece<T>::N;
+    const int r = blockIdx.x / parts, part = blockIdx.x - r * parts;
+    const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
+    T *out = static_cast<T *>(a.dlogits) + (size_t)r * a.ldd;
     const int token = a.g_lp ? a.tokens[r] : -1;
     const bool given = token >= 0 && token < a.vocab;
     const float g = given ? a.g_lp[r] : 0.f, h = a.g_h ? a.g_h[r] : 0.f, lse = a.lse_in[r];
     const float H = a.g_h ? a.entropy_in[r] : 0.f;
-    const bool zero = (g == 0.f && h == 0.f) || lse == NEG_INF;
-    // t = (x - from) scale - off; from the row itself where lse has no digits left for p
-    float from = 0.f, off = lse;
-    const bool again = !zero && fabsf(lse) >= LSE_LARGE;
-    if (again) {
-        float m = NEG_INF, S = 0.f;
+    const bool zero = (g == 0.f && h == 0.f) || lse == -INF;
+    // of t = log p = scale x - lse
+    const auto gradient = [&](float t, bool token_here) {
+        const float p = fast_exp2(t * LOG2E);
+        float v = -g;
+        if (a.g_h)
+            v = fmaf(-h, fmaxf(t, T_FLOOR) + H, v);
+        v *= p;
+        if (token_here) // 1 - p without the digits that p near 1 would take
+            v = -g * expm1f(t) - p * h * (fmaxf(t, T_FLOOR) + H);
+        return v * a.scale;
+    };
+    if (!zero && fabsf(lse) >= LSE_LARGE) {
+        // from the row itself: one block, so that dlogits may be logits
+        if (part != 0)
+            return;
+        float m = -INF, S = 0.f;
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
-            m = fmaxf(m, to_f32(x[j]));
-        from = block_join(m, [](float p, float q) { return fmaxf(p, q); });
+            m = fmaxf(m, to_f32(row[j]));
+        m = block_join(m, [](float p, float q) { return fmaxf(p, q); });
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
-            S += exp2f((to_f32(x[j]) - from) * a.scale * LOG2E);
-        off = logf(block_join(S, [](float p, float q) { return p + q; }));
+            S += fast_exp2((to_f32(row[j]) - m) * a.scale * LOG2E);
+        const float logS = logf(block_join(S, [](float p, float q) { return p + q; }));
+        for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
+            from_f32(out + j, gradient((to_f32(row[j]) - m) * a.scale - logS, j == token));
+        return;
     }
-    for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
-        float v = 0.f;
-        if (!zero) {
-            const float xj = to_f32(x[j]);
-            const float t = again ? (xj - from) * a.scale - off : fmaf(xj, a.scale, -off), p = exp2f(t * LOG2E);
-            v = p * (-g - h * (fmaxf(t, T_FLOOR) + H));
-            if (j == token) // 1 - p without the digits that p near 1 would take
-                v = -g * expm1f(t) - p * h * (fmaxf(t, T_FLOOR) + H);
+    const int before = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
+    const bool alike = reinterpret_cast<uintptr_t>(out) % 16 / sizeof(T) == before;
+    const int pieces = (before + a.vocab + N - 1) / N;
+    const int first = part * BWD_PIECES * LP_THREADS + threadIdx.x;
+    Piece<T> p[BWD_PIECES];
+    if (!zero) {
+#pragma unroll
+        for (int u = 0; u < BWD_PIECES; ++u)
+            if (first + u * LP_THREADS < pieces)
+                p[u].v = *reinterpret_cast<const uint4 *>(row - before + (size_t)(first + u * LP_THREADS) * N);
+    }
+#pragma unroll
+    for (int u = 0; u < BWD_PIECES; ++u) {
+        const int i = first + u * LP_THREADS, id = i * N - before;
+        if (i >= pieces)
+            break;
+        float v[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            v[e] = zero ? 0.f : gradient(fmaf(p[u].get(e), a.scale, -lse), false);
+        if ((unsigned)(token - id) < (unsigned)N && !zero) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (id + e == token)
+                    v[e] = gradient(fmaf(p[u].get(e), a.scale, -lse), true);
         }
-        from_f32(d + j, v * a.scale);
+        if (alike && id >= 0 && id + N <= a.vocab) {
+            uint4 w;
+            if constexpr (sizeof(T) == 4)
+                w = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+            else
+                w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
+                               pack_bf16x2(v[6], v[7]));
+            *reinterpret_cast<uint4 *>(out + id) = w;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (id + e >= 0 && id + e < a.vocab)
+                    from_f32(out + id + e, v[e]);
+        }
     }
+}
+
+template <class T, bool ENTROPY, bool TOP>
+void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
+{
+    const auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
+    const size_t smem = TOP ? (CHUNK + LONG_LIST) * sizeof(uint64_t) : 0;
+    // few rows are cut as long as the GPU has places left and a part keeps a chunk
+    int parts = 1;
+    while (parts < MAX_CLUSTER && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= CHUNK)
+        parts *= 2;
+    const int part_len = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = parts;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3((unsigned)a.rows * parts);
+    cfg.blockDim = dim3(LP_THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cfg.attrs = at;
+    cfg.numAttrs = parts > 1 ? 1 : 0;
+    cudaLaunchKernelEx(&cfg, kernel, a, parts, part_len);
+}
+
+template <class T>
+void forward_of(const LogprobArgs &a, int n_sm, cudaStream_t s)
+{
+    if (a.top_k)
+        a.entropy ? forward<T, true, true>(a, n_sm, s) : forward<T, false, true>(a, n_sm, s);
+    else
+        a.entropy ? forward<T, true, false>(a, n_sm, s) : forward<T, false, false>(a, n_sm, s);
+}
+
+template <class T>
+int backward_of(const LogprobArgs &a, cudaStream_t s)
+{
+    // a row that begins inside a piece may take one more
+    const int64_t pieces = ((int64_t)a.vocab + 2 * Piece<T>::N - 2) / Piece<T>::N;
+    const int parts = (int)((pieces + BWD_PIECES * LP_THREADS - 1) / (BWD_PIECES * LP_THREADS));
+    if ((int64_t)a.rows * parts > INT32_MAX)
+        return PEAGLE_ERR_TOO_LARGE;
+    logprobs_bwd_kernel<T><<<(unsigned)a.rows * parts, LP_THREADS, 0, s>>>(a, parts);
+    return 1;
 }
 
 } // namespace
 
 int launch_logprobs_fwd(const LogprobArgs &a, int n_sm, cudaStream_t s)
 {
-    (void)n_sm;
-    if (a.dtype == PEAGLE_F32)
-        logprobs_fwd_rows<float><<<a.rows, LP_THREADS, 0, s>>>(a);
-    else
-        logprobs_fwd_rows<__nv_bfloat16><<<a.rows, LP_THREADS, 0, s>>>(a);
+    a.dtype == PEAGLE_F32 ? forward_of<float>(a, n_sm, s) : forward_of<__nv_bfloat16>(a, n_sm, s);
     return 1;
 }
 
 int launch_logprobs_bwd(const LogprobArgs &a, int n_sm, cudaStream_t s)
 {
     (void)n_sm;
-    if (a.dtype == PEAGLE_F32)
-        logprobs_bwd_rows<float><<<a.rows, LP_THREADS, 0, s>>>(a);
-    else
-        logprobs_bwd_rows<__nv_bfloat16><<<a.rows, LP_THREADS, 0, s>>>(a);
-    return 1;
+    return a.dtype == PEAGLE_F32 ? backward_of<float>(a, s) : backward_of<__nv_bfloat16>(a, s);
 }
 
 } // namespace peagle

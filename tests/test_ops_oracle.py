@@ -226,7 +226,7 @@ def _logprob_call(lib, ctx, back, **over):
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("over,status", [
     ({"rows": 0}, "OK"), ({"rows": -2}, "BAD_SHAPE"), ({"vocab": 0}, "BAD_SHAPE"), ({"ld": 99}, "BAD_SHAPE"),
-    ({"dtype": 5}, "BAD_SHAPE"), ({"scale": 0.0}, "BAD_SHAPE"), ({"scale": -1.0}, "BAD_SHAPE"),
+    ({"dtype": 5}, "BAD_SHAPE"), ({"vocab": (1 << 30) + 1, "ld": 1 << 31, "ldd": 1 << 31}, "TOO_LARGE"), ({"scale": 0.0}, "BAD_SHAPE"), ({"scale": -1.0}, "BAD_SHAPE"),
     ({"scale": float("nan")}, "BAD_SHAPE"), ({"scale": float("inf")}, "BAD_SHAPE"), ({"logits": 0}, "NULL"),
     ({"tokens": 0}, "NULL"), ({"logits": 4097}, "ALIGN"), ({"tokens": 8194}, "ALIGN"), ({"lse": 16386}, "ALIGN"),
 ])
