@@ -12,10 +12,11 @@
 // rows are cut into parts for a cluster of up to 8 blocks, which join through distributed shared memory.
 //
 // Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
-// k-th largest of the threads' maxima, then the k-th best entry so far).  A chunk's maximum, which the sums need
-// anyway, says whether it holds anything to add; what reaches the bound goes to a list in shared memory, with room
-// for a whole chunk, and a long list is cut to its k best.  Entries are compared by value, then by id, so the result
-// does not depend on the order in which they came.
+// k-th largest of the maxima of 64 groups of threads, then the k-th best entry so far).  A chunk's maximum, which the
+// sums need anyway, says whether a thread has anything to add; what reaches the bound goes to a list in shared memory,
+// which is cut to its k best when it has grown by half.  A chunk that does not fit the list (rows in ascending order, or of
+// equal entries) is gone through again with the bound that the list gives.  Entries are compared by value, then by id,
+// so the result does not depend on the order in which they came.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -28,12 +29,18 @@ using namespace sm100;
 
 namespace {
 
-constexpr int LP_THREADS = 256, LP_WARPS = LP_THREADS / 32;
-constexpr int CHUNK = 4096;      // entries per chunk
-constexpr int LONG_LIST = 256;   // a list longer than this is cut down between chunks
-constexpr int COUNTED = 2 * LP_THREADS; // entries that are ranked by counting, at most
+// Blocks of 128 threads: 4,096 rows of 128,000 bf16 with 8 alternatives take 252 us, with blocks of 256 (the same
+// threads per SM, but more of them at a barrier) 271; 8 blocks to an SM, with 10 the registers do not suffice.
+constexpr int LP_THREADS = 128, LP_WARPS = LP_THREADS / 32;
+constexpr int FWD_PIECES = 4; // 16-byte pieces per thread and chunk
+constexpr int GROUPS = 64;     // of threads, whose maxima give the first bound
+constexpr int STAGES = 2;     // chunks on their way or at hand
+constexpr int LIST = 1024;    // entries of the list of candidates
+constexpr int COUNTED = 512; // entries that are ranked by counting, at most
 constexpr int MAX_CLUSTER = 8;
-static_assert(MAX_CLUSTER * PEAGLE_MAX_TOP_K <= COUNTED, "the lists of a cluster are ranked at once");
+constexpr int LEAST_PART = 4096; // entries of a row's part
+static_assert(GROUPS >= PEAGLE_MAX_TOP_K && LP_THREADS % GROUPS == 0, "a first bound for every k");
+static_assert(MAX_CLUSTER * PEAGLE_MAX_TOP_K <= COUNTED && COUNTED <= LIST, "the lists of a cluster are ranked at once");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float T_FLOOR = -300.f; // below this, in powers of two, a probability is zero in fp32
 constexpr float LSE_LARGE = 8192.f; // from here on fp32 keeps less than 2^-10 of a log-sum-exp
@@ -88,7 +95,7 @@ __device__ __forceinline__ float reference(float m, float l)
 __device__ __forceinline__ void rescale(Sums &s, float m, float l)
 {
     if (s.m != -INF && s.m != m) {
-        const float d = reference(s.m, l) - reference(m, l), f = exp2f(d);
+        const float d = reference(s.m, l) - reference(m, l), f = fast_exp2(d);
         s.E = f * fmaf(s.S, fmaxf(d, T_FLOOR), s.E);
         s.S *= f;
     }
@@ -147,21 +154,29 @@ __device__ __forceinline__ void write_row(const LogprobArgs &a, int r, const Row
 
 // ------------------------------------------------------------------ lists of the best entries
 
-// Sorts a list and cuts it to its k best.  The whole block; a barrier before and after.  Returns the new length.
-__device__ __forceinline__ int cut_list(uint64_t *list, int n, int k)
+// The k-th best of n >= k entries, bit by bit.  The whole block; a barrier after.
+__device__ __noinline__ uint64_t kth_best(const uint64_t *list, int n, int k)
+{
+    uint64_t bound = 0;
+    for (int bit = 63; bit >= 0; --bit) {
+        const uint64_t trial = bound | 1ull << bit;
+        int c = 0;
+        for (int i = threadIdx.x; i < n; i += LP_THREADS)
+            c += list[i] >= trial;
+        if (block_join(c, [](int p, int q) { return p + q; }) >= k)
+            bound = trial;
+    }
+    __syncthreads();
+    return bound;
+}
+
+// Sorts a list and cuts it to its k best; an entry of 0 is none.  The whole block; a barrier before and after.
+__device__ __noinline__ void cut_list(uint64_t *list, int n, int k)
 {
     __shared__ uint64_t kept[PEAGLE_MAX_TOP_K];
     __shared__ int kept_n;
-    if (n > COUNTED) { // the k-th best entry bit by bit, then what is not below it
-        uint64_t bound = 0;
-        for (int bit = 63; bit >= 0; --bit) {
-            const uint64_t trial = bound | 1ull << bit;
-            int c = 0;
-            for (int i = threadIdx.x; i < n; i += LP_THREADS)
-                c += list[i] >= trial;
-            if (block_join(c, [](int p, int q) { return p + q; }) >= k)
-                bound = trial;
-        }
+    if (n > COUNTED) {
+        const uint64_t bound = kth_best(list, n, k);
         if (threadIdx.x == 0)
             kept_n = 0;
         __syncthreads();
@@ -175,23 +190,35 @@ __device__ __forceinline__ int cut_list(uint64_t *list, int n, int k)
         __syncthreads();
     }
     // an entry's place is the number of better ones
-    uint64_t mine[2];
-    int place[2] = {0, 0};
+    constexpr int EACH = COUNTED / LP_THREADS;
+    uint64_t mine[EACH];
+    int place[EACH];
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < EACH; ++j) {
         const int i = threadIdx.x + j * LP_THREADS;
         mine[j] = i < n ? list[i] : 0;
-        if (mine[j])
+        place[j] = 0;
+    }
+    if (n <= LP_THREADS) {
+        if (mine[0])
+#pragma unroll 4
             for (int o = 0; o < n; ++o)
-                place[j] += list[o] > mine[j];
+                place[0] += list[o] > mine[0];
+    } else {
+#pragma unroll 4
+        for (int o = 0; o < n; ++o) {
+            const uint64_t other = list[o];
+#pragma unroll
+            for (int j = 0; j < EACH; ++j)
+                place[j] += other > mine[j];
+        }
     }
     __syncthreads();
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < EACH; ++j)
         if (mine[j] && place[j] < k)
             list[place[j]] = mine[j];
     __syncthreads();
-    return min(n, k);
 }
 
 __device__ __forceinline__ uint64_t load_remote(const uint64_t *p, uint32_t rank)
@@ -214,12 +241,6 @@ template <class T>
 struct Piece {
     static constexpr int N = 16 / sizeof(T);
     uint4 v;
-    __device__ __forceinline__ void load(const T *p)
-    {
-        asm("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-            : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-            : "l"(p));
-    }
     __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
     __device__ __forceinline__ float get(int e) const
     {
@@ -243,31 +264,57 @@ struct Piece {
         v = make_uint4(w[0], w[1], w[2], w[3]);
     }
 };
-__device__ __forceinline__ float piece_max(const Piece<float> &p, float m)
-{
-    return max3(max3(m, p.get(0), p.get(1)), p.get(2), p.get(3));
-}
+// The largest entries of a piece, as one word: a number, or one of the even and one of the odd entries.
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b)
 {
     uint32_t r;
     asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
-__device__ __forceinline__ float piece_max(const Piece<__nv_bfloat16> &p, float m)
+__device__ __forceinline__ uint32_t piece_max(const Piece<float> &p)
 {
-    const uint32_t w = max_bf16x2(max_bf16x2(p.v.x, p.v.y), max_bf16x2(p.v.z, p.v.w));
-    return max3(m, __uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+    return __float_as_uint(fmaxf(max3(p.get(0), p.get(1), p.get(2)), p.get(3)));
+}
+__device__ __forceinline__ uint32_t piece_max(const Piece<__nv_bfloat16> &p)
+{
+    return max_bf16x2(max_bf16x2(p.v.x, p.v.y), max_bf16x2(p.v.z, p.v.w));
+}
+template <class T>
+__device__ __forceinline__ uint32_t max_words(uint32_t a, uint32_t b)
+{
+    if constexpr (sizeof(T) == 4)
+        return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    else
+        return max_bf16x2(a, b);
+}
+template <class T>
+__device__ __forceinline__ float of_max_word(uint32_t w)
+{
+    if constexpr (sizeof(T) == 4)
+        return fmaxf(__uint_as_float(w), -INF); // a piece of nothing but NaN has no maximum
+    else
+        return max3(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u), -INF);
+}
+
+// Two bf16 entries that are no less than `low`, a NaN as it is.
+__device__ __forceinline__ uint32_t raised(uint32_t w, uint32_t low)
+{
+    uint32_t r;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(low));
+    return r;
 }
 
 // A block per part of a row; `parts` blocks, a cluster, have a row.  part_len is a multiple of 8.
 template <class T, bool ENTROPY, bool TOP>
-__global__ void __launch_bounds__(LP_THREADS, 4)
+__global__ void __launch_bounds__(LP_THREADS, 8)
     logprobs_fwd_kernel(const __grid_constant__ LogprobArgs a, int parts, int part_len)
 {
-    constexpr int N = Piece<T>::N, U = CHUNK / (LP_THREADS * N);
-    extern __shared__ uint64_t list[]; // TOP: CHUNK + LONG_LIST entries
-    __shared__ int count;
-    __shared__ float4 first_max[LP_THREADS / 4];
+    constexpr int N = Piece<T>::N, U = FWD_PIECES, STEP = U * LP_THREADS;
+    // a thread's pieces wait in its own places: no barrier between their arrival and their use
+    extern __shared__ uint4 ring[]; // [STAGES][U][LP_THREADS]
+    __shared__ uint64_t list[TOP ? LIST : 1];
+    __shared__ int count; // entries that came to the list; those past its end have been dropped
+    __shared__ float4 first_max[TOP ? GROUPS / 4 : 1];
     __shared__ float first_bound;
     __shared__ Sums warp_sums[LP_WARPS], sums;
     __shared__ RowStats stats;
@@ -276,96 +323,189 @@ __global__ void __launch_bounds__(LP_THREADS, 4)
     const T *row = static_cast<const T *>(a.logits) + (size_t)r * a.ld;
     // whole 16-byte pieces that hold an entry of this part; `before` entries of the first belong elsewhere
     const int before = (int)(reinterpret_cast<uintptr_t>(row + begin) % 16 / sizeof(T));
-    const T *x = row + begin - before;
     const int pieces = n ? (before + n + N - 1) / N : 0;
+    const T *x = row + begin - before + threadIdx.x * N; // this thread's first piece of the next chunk to be fetched
     const float l = a.scale * LOG2E;
-    const int token = a.tokens && part == 0 ? a.tokens[r] : -1;
+    const uint32_t ring_at = smem_u32(ring + threadIdx.x);
 
-    const auto load = [&](Piece<T> (&p)[U], int first) {
+    const auto fetch = [&](int first, int stage) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int i = first + u * LP_THREADS + threadIdx.x;
-            if (i < pieces)
-                p[u].load(x + (size_t)i * N);
-            if (i == 0 || i >= pieces - 1)
-                p[u].mask(i < pieces ? before - i * N : N, before + n - i * N);
-        }
+        for (int u = 0; u < U; ++u)
+            if (first + u * LP_THREADS + (int)threadIdx.x < pieces)
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ring_at + (stage * U + u) * LP_THREADS * 16),
+                             "l"(x + u * LP_THREADS * N)
+                             : "memory");
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        x += STEP * N;
     };
-    Piece<T> now[U], next[U];
-    load(now, 0);
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i)
+        fetch(i * STEP, i);
     if (TOP && threadIdx.x == 0)
         count = 0;
     Sums s = {-INF, 0.f, 0.f};
-    float bound = -INF;  // an entry at or above it may be among the k best
-    for (int first = 0; first < pieces; first += U * LP_THREADS) {
-        if (first + U * LP_THREADS < pieces)
-            load(next, first + U * LP_THREADS);
-        float top = -INF;
+    float bound = -INF; // an entry at or above it may be among the k best
+    int stage = 0;
+    for (int first = 0; first < pieces; first += STEP) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+        const uint4 *at = ring + stage * STEP + threadIdx.x;
+        Piece<T> now[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            top = piece_max(now[u], top);
+            now[u].v = at[u * LP_THREADS];
+        if (first == 0 || first + STEP >= pieces) { // with the first piece, the last, or none
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = first + u * LP_THREADS + threadIdx.x;
+                if (i == 0 || i >= pieces - 1)
+                    now[u].mask(i < pieces ? before - i * N : N, before + n - i * N);
+            }
+        }
+        uint32_t most[U], all = piece_max(now[0]);
+        most[0] = all;
+#pragma unroll
+        for (int u = 1; u < U; ++u) {
+            most[u] = piece_max(now[u]);
+            all = max_words<T>(all, most[u]);
+        }
+        const float top = of_max_word<T>(all);
         if (top > s.m)
             rescale(s, top, l);
         const float c = reference(s.m, l);
+        // Entries whose probability is zero in any case are raised to where 0 times their t is 0: as pairs of bf16
+        // here, else one by one.  The second term is more than the rounding to bf16 takes off.  (Beside a maximum
+        // near the end of the type's range there is no room for that: see below.)
+        const float from = s.m == -INF ? 0.f : s.m;
+        const float low = fabsf(from) < 1e37f ? fmaf(fabsf(from), -0x1p-6f, from + T_FLOOR / l) : -INF;
+        const uint32_t low2 = pack_bf16x2(low, low);
         const F2 l2 = f2(l, l), minus = f2(-c, -c);
         F2 S2 = f2(s.S, 0.f), E2 = f2(s.E, 0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int e = 0; e < N; e += 2) {
-                const F2 t = fma_f2(f2(now[u].get(e), now[u].get(e + 1)), l2, minus);
+                F2 v;
+                if constexpr (ENTROPY && N == 8) {
+                    const uint32_t w = raised(now[u].word(e / 2), low2);
+                    v = f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+                } else {
+                    v = f2(now[u].get(e), now[u].get(e + 1));
+                }
+                F2 t = fma_f2(v, l2, minus);
                 const float2 tv = unf2(t);
                 const F2 p = f2(fast_exp2(tv.x), fast_exp2(tv.y));
                 S2 = add_f2(S2, p);
+                if (ENTROPY && N == 4)
+                    t = f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR));
                 if (ENTROPY)
-                    E2 = fma_f2(p, f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR)), E2);
+                    E2 = fma_f2(p, t, E2);
             }
         const float2 Sv = unf2(S2), Ev = unf2(E2);
         s.S = Sv.x + Sv.y;
-        s.E = Ev.x + Ev.y;
-        if (TOP) {
-            if (first == 0) { // the k-th largest of the threads' maxima
-                reinterpret_cast<float *>(first_max)[threadIdx.x] = top;
-                __syncthreads();
-                int above = 0, equal = 0;
-#pragma unroll 8
-                for (int i = 0; i < LP_THREADS / 4; ++i) {
-                    const float4 o = first_max[i];
-                    above += (o.x > top) + (o.y > top) + (o.z > top) + (o.w > top);
-                    equal += (o.x == top) + (o.y == top) + (o.z == top) + (o.w == top);
+        if constexpr (ENTROPY && N == 8) {
+            const float E = Ev.x + Ev.y;
+            if (E != E && s.S == s.S) {
+#pragma unroll 1
+                for (int i = 0; i < U * N; ++i) {
+                    const int id = (first + i / N * LP_THREADS + (int)threadIdx.x) * N + i % N - before;
+                    const float t = fmaf(to_f32(reinterpret_cast<const T *>(at + i / N * LP_THREADS)[i % N]), l, -c);
+                    if (id >= 0 && id < n)
+                        s.E = fmaf(fast_exp2(t), fmaxf(t, T_FLOOR), s.E);
                 }
-                if (above < a.top_k && above + equal >= a.top_k)
-                    first_bound = top;
+            } else {
+                s.E = E;
+            }
+        } else {
+            s.E = Ev.x + Ev.y;
+        }
+        if constexpr (TOP) {
+            const int k = a.top_k;
+            if (first == 0) { // the k-th largest of the maxima of 64 groups of threads
+                constexpr int LANES = LP_THREADS / GROUPS;
+                float most = top;
+#pragma unroll
+                for (int o = 1; o < LANES; o *= 2)
+                    most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                if (threadIdx.x % LANES == 0)
+                    reinterpret_cast<float *>(first_max)[threadIdx.x / LANES] = most;
+                __syncthreads();
+                if (threadIdx.x < GROUPS) {
+                    most = reinterpret_cast<float *>(first_max)[threadIdx.x];
+                    int above = 0, equal = 0;
+#pragma unroll
+                    for (int i = 0; i < GROUPS / 4; ++i) {
+                        const float4 o = first_max[i];
+                        above += (o.x > most) + (o.y > most) + (o.z > most) + (o.w > most);
+                        equal += (o.x == most) + (o.y == most) + (o.z == most) + (o.w == most);
+                    }
+                    if (above < k && above + equal >= k)
+                        first_bound = most;
+                }
                 __syncthreads();
                 bound = first_bound;
             }
-            int end = 0;
-            if (top >= bound) {
+            uint64_t least = 0;
+            while (true) {
+                int end = 0;
+                if (top >= bound) {
+                    // which of the entries reach the bound, without a branch among a piece's: a thread on this path
+                    // keeps its whole block waiting
+                    uint32_t reach = 0;
 #pragma unroll
-                for (int u = 0; u < U; ++u)
+                    for (int u = 0; u < U; ++u)
+                        if (of_max_word<T>(most[u]) >= bound) {
+                            Piece<T> p;
+                            p.v = at[u * LP_THREADS];
 #pragma unroll
-                    for (int e = 0; e < N; ++e) {
-                        const float v = now[u].get(e);
-                        const int id = (first + u * LP_THREADS + threadIdx.x) * N + e - before;
-                        if (v >= bound && id >= 0 && id < n) {
-                            end = atomicAdd(&count, 1);
-                            list[end++] = rank_key(v, begin + id);
+                            for (int e = 0; e < N; ++e)
+                                reach |= (uint32_t)(p.get(e) >= bound) << (u * N + e);
+                        }
+                    for (; reach; reach &= reach - 1) {
+                        const int i = __ffs(reach) - 1, u = i / N, e = i % N;
+                        const int id = (first + u * LP_THREADS + (int)threadIdx.x) * N + e - before;
+                        const float v = to_f32(reinterpret_cast<const T *>(at + u * LP_THREADS)[e]);
+                        const uint64_t key = rank_key(v, begin + id);
+                        if (id >= 0 && id < n && key >= least) {
+                            const int place = atomicAdd(&count, 1);
+                            if (place < LIST)
+                                list[place] = key;
+                            end = place + 1;
                         }
                     }
-            }
-            if (first == 0)
-                bound = from_key(order_key(bound) + 1); // k entries with lower ids reach it
-            if (__syncthreads_or(end > LONG_LIST)) {
-                cut_list(list, count, a.top_k);
-                if (threadIdx.x == 0)
-                    count = a.top_k;
-                bound = from_key((uint32_t)(list[a.top_k - 1] >> 32) + 1);
+                }
+                if (!__syncthreads_or(end > k + k / 2 + 6)) {
+                    if (first == 0)
+                        bound = from_key(order_key(bound) + 1); // k entries of this chunk, with lower ids, reach it
+                    break;
+                }
+                if (count <= LIST) {
+                    cut_list(list, count, k);
+                    if (threadIdx.x == 0)
+                        count = k;
+                    bound = from_key((uint32_t)(list[k - 1] >> 32) + 1); // the k best have lower ids than what follows
+                    __syncthreads();
+                    break;
+                }
+                // once more, for what reaches the k-th best of those that found a place
+                least = kth_best(list, LIST, k);
+                uint64_t mine[LIST / LP_THREADS];
+#pragma unroll
+                for (int j = 0; j < LIST / LP_THREADS; ++j)
+                    mine[j] = list[threadIdx.x + j * LP_THREADS];
                 __syncthreads();
+                if (threadIdx.x == 0)
+                    count = 0;
+                __syncthreads();
+                const int chunk_id = begin + first * N - before;
+#pragma unroll
+                for (int j = 0; j < LIST / LP_THREADS; ++j)
+                    if (mine[j] >= least && (int)~(uint32_t)mine[j] < chunk_id) // from the chunks before
+                        list[atomicAdd(&count, 1)] = mine[j];
+                bound = from_key((uint32_t)(least >> 32));
             }
         }
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-            now[u] = next[u];
+        fetch(first + STAGES * STEP, stage);
+        stage = stage + 1 == STAGES ? 0 : stage + 1;
     }
 
     // join the threads' sums, then the blocks'
@@ -376,42 +516,48 @@ __global__ void __launch_bounds__(LP_THREADS, 4)
     if ((threadIdx.x & 31) == 0)
         warp_sums[threadIdx.x >> 5] = s;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        s = warp_sums[0];
-        for (int i = 1; i < LP_WARPS; ++i)
-            s = join(s, warp_sums[i], l);
-        sums = s;
+    if (threadIdx.x < 32) {
+        s = warp_sums[threadIdx.x % LP_WARPS];
+        for (int o = LP_WARPS / 2; o; o >>= 1) {
+            const Sums other = {__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.S, o), __shfl_xor_sync(~0u, s.E, o)};
+            s = join(s, other, l);
+        }
+        if (threadIdx.x == 0)
+            sums = s;
     }
-    int have = 0;
-    if (TOP)
-        have = cut_list(list, count, a.top_k);
-    if (parts > 1) {
-        if (TOP && threadIdx.x >= have && threadIdx.x < a.top_k)
+    if (TOP) {
+        const int held = count;
+        cut_list(list, held, a.top_k);
+        if ((int)threadIdx.x >= held && threadIdx.x < a.top_k)
             list[threadIdx.x] = 0;
+    }
+    if (parts > 1) {
         cluster_sync_all();
         if (part == 0) {
             if (threadIdx.x == 0)
                 for (int p = 1; p < parts; ++p)
                     s = join(s, {load_remote(&sums.m, p), load_remote(&sums.S, p), load_remote(&sums.E, p)}, l);
             if (TOP) {
-                uint64_t theirs[MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS];
+                const int k = a.top_k;
+                uint64_t theirs[COUNTED / LP_THREADS];
 #pragma unroll
-                for (int j = 0; j < MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS; ++j) {
+                for (int j = 0; j < COUNTED / LP_THREADS; ++j) {
                     const int i = threadIdx.x + j * LP_THREADS;
-                    theirs[j] = i < parts * a.top_k ? load_remote(&list[i % a.top_k], i / a.top_k) : 0;
+                    theirs[j] = i < parts * k ? load_remote(&list[i % k], i / k) : 0;
                 }
                 __syncthreads();
 #pragma unroll
-                for (int j = 0; j < MAX_CLUSTER * PEAGLE_MAX_TOP_K / LP_THREADS; ++j)
+                for (int j = 0; j < COUNTED / LP_THREADS; ++j)
                     list[threadIdx.x + j * LP_THREADS] = theirs[j];
                 __syncthreads();
-                have = cut_list(list, parts * a.top_k, a.top_k);
+                cut_list(list, parts * k, k);
             }
         }
         cluster_sync_all(); // nobody leaves while its lists are read
         if (part != 0)
             return;
     }
+    const int token = a.tokens ? a.tokens[r] : -1;
     const float x_token = token >= 0 && token < a.vocab ? to_f32(row[token]) : 0.f;
     if (threadIdx.x == 0) {
         sums = s;
@@ -536,10 +682,9 @@ template <class T, bool ENTROPY, bool TOP>
 void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
 {
     const auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
-    const size_t smem = TOP ? (CHUNK + LONG_LIST) * sizeof(uint64_t) : 0;
-    // few rows are cut as long as the GPU has places left and a part keeps a chunk
+    // few rows are cut as long as the GPU has places left
     int parts = 1;
-    while (parts < MAX_CLUSTER && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= CHUNK)
+    while (parts < MAX_CLUSTER && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
         parts *= 2;
     const int part_len = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};
@@ -549,7 +694,7 @@ void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)a.rows * parts);
     cfg.blockDim = dim3(LP_THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = STAGES * FWD_PIECES * LP_THREADS * 16;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;
