@@ -145,7 +145,7 @@ def block_scale(x, block=256):
 
 def stochastic_code(y, bits16, keep):
     """e4m3 code below or above y (|y| <= 256), the upper one if the fraction between them, in 2^-20, plus the 16
-    random bits (as 2^-20 (16 bits + 1/2)) reaches one."""
+    random bits (as 2^-20 (16 bits + 1/2)) reaches one; and how far y is from where that changes."""
     values = e4m3_values()[:127]
     a = np.abs(y)
     finite = a <= 256
@@ -153,34 +153,40 @@ def stochastic_code(y, bits16, keep):
     low = np.clip(np.searchsorted(values, a, side="right") - 1, 0, 125)
     span = values[low + 1] - values[low]
     fraction = np.floor((a - values[low]) / span * 2 ** 20)
-    code = low + (fraction + bits16 * 16.0 + 8 >= 2 ** 20)
+    rest = fraction + bits16 * 16.0 + 8 - 2 ** 20
+    code = low + (rest >= 0)
+    # the border above, or that of the number's own interval from below
+    margin = np.minimum(np.abs(rest), fraction) * span / 2 ** 20
     if keep:
         code = np.where((y > 0) & (code == 0), 1, code)
-    return np.where(finite, code + np.where(np.signbit(y), 128, 0), 127).astype(np.uint8)
+    return np.where(finite, code + np.where(np.signbit(y), 128, 0), 127).astype(np.uint8), margin
 
 
 def adamw_states8(g, m_code, v_code, m_scale, v_scale, beta1, beta2, seed, step, place):
-    """fp32 m and root that the step uses, and the new codes and scales, bit for bit."""
+    """fp32 m and root that the step uses, the new codes, how far m and root are from where their codes change (fp32
+    arithmetic may land on the other side), and the new scales."""
     n = len(g)
     per = lambda s: np.repeat(np.asarray(s, np.float64), 256)[:n]
     value = e4m3_values()
     g = np.asarray(g, np.float64)
-    m = (beta1 * (value[m_code] * per(m_scale)) + (1 - beta1) * g).astype(np.float32)
-    v0 = (np.float32(value[v_code] * per(v_scale)) ** 2).astype(np.float64)
     with np.errstate(over="ignore", invalid="ignore"):
+        m = (beta1 * (value[m_code] * per(m_scale)) + (1 - beta1) * g).astype(np.float32)
+        v0 = (np.float32(value[v_code] * per(v_scale)) ** 2).astype(np.float64)
         v = (beta2 * v0 + ((1 - beta2) * g) * g).astype(np.float32)
         root = np.sqrt(v)
     bits = adamw_random_bits(seed, step, place, n)
     ms, vs = block_scale(m.astype(np.float64)), block_scale(root.astype(np.float64))
-    # numbers below 2^-6 get 2^-6 added in fp32 before their fraction is taken, which rounds them to 2^-29
+
     def scaled(x, s):
+        # numbers below 2^-6 get 2^-6 added in fp32 before their fraction is taken, which rounds them to 2^-29
         y = x.astype(np.float64) / per(s)
         small = np.abs(y) < 2.0 ** -6
         with np.errstate(invalid="ignore"):
             z = (np.float32(np.abs(y)) + np.float32(2.0 ** -6)).astype(np.float64) - 2.0 ** -6
         return np.where(small, np.copysign(z, y), y)
-    new_m = stochastic_code(scaled(m, ms), (bits & np.uint64(0xFFFF)).astype(np.float64), False)
+
+    new_m, off_m = stochastic_code(scaled(m, ms), (bits & np.uint64(0xFFFF)).astype(np.float64), False)
     r = scaled(root, vs)
-    new_v = stochastic_code(np.where(root > 0, np.maximum(r, 2.0 ** -30), r) if n else r,
-                            (bits >> np.uint64(16)).astype(np.float64), True)
-    return m, root, new_m, new_v, ms, vs
+    new_v, off_v = stochastic_code(np.where(root > 0, np.maximum(r, 2.0 ** -30), r) if n else r,
+                                   (bits >> np.uint64(16)).astype(np.float64), True)
+    return m, root, new_m, new_v, off_m * per(ms), off_v * per(vs), ms, vs

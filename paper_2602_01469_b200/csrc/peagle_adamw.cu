@@ -11,8 +11,13 @@
 // 8-bit states: a warp has the 256 elements that share a scale.  m and sqrt(v) are e4m3 codes times a power of two,
 // so scaling is exact and the rounding to a code looks at the fp32 number's own bits: adding 20 random bits below
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
-// (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first.)  The new m and v are formed in fp64 and
-// rounded once to fp32, so that the codes do not depend on how the arithmetic is ordered.
+// (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
+// bounds this is instructions, about 70 per element and half of them integer ones for the random bits and the
+// roundings, and the wait for memory with registers for no more than four blocks.  The first version had 113: it
+// formed the new m and v in fp64 so that the codes would not depend on how the arithmetic is ordered.  In fp32 two or
+// three codes in a million fall on the other side of the random bits, which is as good a rounding; only a block's
+// scale has to be right, and where a block's largest number lies at a power of two, or is not finite, the largest is
+// found again in fp64.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -22,12 +27,15 @@
 #include "sm100_ptx.cuh"
 
 namespace peagle {
+using namespace sm100;
 
 namespace {
 
 constexpr int AW_THREADS = 256;
 constexpr int AW_BLOCK = PEAGLE_ADAMW_BLOCK;
-constexpr int CHUNK = (AW_THREADS / 32) * AW_BLOCK; // elements per thread block
+// Elements per thread block, 8 per thread.  (Blocks that go on to a second and third 2,048 spend fewer instructions on
+// finding their tensor and wait longer for memory: 8-bit states of 91 M elements 254 us, with two 300, with four 283.)
+constexpr int CHUNK = (AW_THREADS / 32) * AW_BLOCK;
 constexpr uint32_t GOLDEN = 0x9E3779B9u;            // 2^32 / golden ratio
 
 struct Tensor {
@@ -134,8 +142,8 @@ __device__ __forceinline__ void store8(void *p, int dtype, int64_t i, int left, 
         __nv_bfloat16 *q = static_cast<__nv_bfloat16 *>(p) + i;
         if (VEC) {
             *reinterpret_cast<uint4 *>(q) =
-                make_uint4(sm100::pack_bf16x2(f[0], f[1]), sm100::pack_bf16x2(f[2], f[3]), sm100::pack_bf16x2(f[4], f[5]),
-                           sm100::pack_bf16x2(f[6], f[7]));
+                make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]),
+                           pack_bf16x2(f[6], f[7]));
         } else {
 #pragma unroll
             for (int k = 0; k < 8; ++k)
@@ -197,17 +205,15 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
     return (uint32_t)hi << 16 | lo;
 }
 
-// y rounded up or down to an e4m3 number, by 16 random bits; |y| <= 256, anything else gives NaN.  `keep`: not to
-// zero (y >= 0).
-__device__ __forceinline__ float to_e4m3(float y, uint32_t bits16, bool keep)
+// y >= 0 rounded up or down to an e4m3 number: `bits20` are 20 random bits.
+__device__ __forceinline__ float to_e4m3(float y, uint32_t bits20)
 {
-    const float a = fabsf(y);
-    const float shift = a < 0.015625f ? 0.015625f : 0.f;
-    float z = __uint_as_float((__float_as_uint(a + shift) + (bits16 << 4) + 8u) & 0xfff00000u) - shift;
-    if (keep)
-        z = fmaxf(z, 0.001953125f); // 2^-9
-    return a <= 256.f ? copysignf(z, y) : __int_as_float(0x7fffffff);
+    const float shift = y < 0.015625f ? 0.015625f : 0.f;
+    return __uint_as_float((__float_as_uint(y + shift) + bits20) & 0xfff00000u) - shift;
 }
+// The 20 bits of an element's random 32 for m and for the root: 16 of them and a half.
+__device__ __forceinline__ uint32_t bits_of_m(uint32_t bits) { return (bits << 4 & 0xffff0u) | 8u; }
+__device__ __forceinline__ uint32_t bits_of_root(uint32_t bits) { return (bits >> 12 & 0xffff0u) | 8u; }
 
 // Power of two that brings `largest` into [128, 256), at least 2^-107; and its reciprocal.
 __device__ __forceinline__ float2 scale_of(float largest)
@@ -216,11 +222,24 @@ __device__ __forceinline__ float2 scale_of(float largest)
     return make_float2(__uint_as_float((uint32_t)(e + 127) << 23), __uint_as_float((uint32_t)(127 - e) << 23));
 }
 
-__device__ __forceinline__ float warp_max(float v)
+__device__ __forceinline__ F2 both(double x) { return f2((float)x, (float)x); }
+__device__ __forceinline__ void put2(float (&to)[8], int k, F2 v)
 {
-    for (int o = 16; o; o >>= 1)
-        v = fmaxf(v, __shfl_xor_sync(~0u, v, o));
-    return v;
+    const float2 u = unf2(v);
+    to[k] = u.x;
+    to[k + 1] = u.y;
+}
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// Whether a block whose largest magnitude has these bits is done over: not finite, or so near a power of two that
+// fp32's roundings may have carried it across.
+__device__ __forceinline__ bool doubtful(uint32_t largest)
+{
+    return largest >= 0x7f800000u || (largest > 0x0e000000u && (largest + 32u & 0x7fffffu) < 64u);
 }
 
 __host__ __device__ inline Factors factors(const How &h, float lr, int64_t step)
@@ -233,86 +252,164 @@ __host__ __device__ inline Factors factors(const How &h, float lr, int64_t step)
     return f;
 }
 
-// One thread's 8 elements of a tensor, from i on; `left` of them are there.  EIGHT: states in 8 bits, a whole warp
-// with a block of PEAGLE_ADAMW_BLOCK elements, the thread's 8 perhaps none.
-template <bool VEC, bool EIGHT>
-__device__ __forceinline__ void step8(const Tensor &t, const How &how, const Factors &f, float grad_scale,
-                                      uint32_t ordinal, int64_t i, int left)
+// Approximate to about two units in the last place; numbers below 2^-126 count as 0.
+__device__ __forceinline__ float root_of(float v)
+{
+    float r;
+    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float quotient(float a, float b)
+{
+    float r;
+    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+// p after a step, two elements; `decay` is -lr weight_decay.
+__device__ __forceinline__ F2 stepped(F2 p, F2 m, F2 root, const How &how, const Factors &f, float decay)
+{
+    const float2 d = unf2(fma_f2(root, f2(f.root_scale, f.root_scale), f2(how.eps, how.eps))), mv = unf2(m);
+    const F2 q = f2(quotient(mv.x, d.x), quotient(mv.y, d.y));
+    return fma_f2(q, f2(-f.step_size, -f.step_size), fma_f2(p, f2(decay, decay), p));
+}
+
+// One thread's 8 elements of a tensor with states in 32 bits, from i on; `left` of them are there.
+template <bool VEC>
+__device__ __forceinline__ void step8(const Tensor &t, const How &how, const Factors &f, float grad_scale, int64_t i, int left)
 {
     float g[8], m[8], v[8], p[8];
-    const int64_t block = i / AW_BLOCK;
-    float ms, vs;
-    uint2 mc, vc;
-    if (EIGHT) {
-        mc = load_codes<VEC>(t.m, i, left);
-        vc = load_codes<VEC>(t.v, i, left);
-        ms = t.m_scale[block];
-        vs = t.v_scale[block];
-    } else {
-        load8<VEC>(t.m, PEAGLE_F32, i, left, m);
-        load8<VEC>(t.v, PEAGLE_F32, i, left, v);
-    }
+    load8<VEC>(t.m, PEAGLE_F32, i, left, m);
+    load8<VEC>(t.v, PEAGLE_F32, i, left, v);
     load8<VEC>(t.grad, t.grad_dtype, i, left, g);
     load8<VEC>(t.master ? t.master : t.param, t.master ? PEAGLE_F32 : t.param_dtype, i, left, p);
-    if (EIGHT) {
-        decode4(mc.x, m, 0);
-        decode4(mc.y, m, 4);
-        decode4(vc.x, v, 0);
-        decode4(vc.y, v, 4);
-    }
-    const float b1 = (float)how.beta1, c1 = (float)(1.0 - how.beta1), b2 = (float)how.beta2, c2 = (float)(1.0 - how.beta2);
-    float m_max = 0.f, r_max = 0.f;
+    const float decay = -f.lr * t.weight_decay;
+    const F2 b1 = both(how.beta1), c1 = both(1.0 - how.beta1), b2 = both(how.beta2), c2 = both(1.0 - how.beta2);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        g[k] *= grad_scale;
-        if (EIGHT) {
-            const float m0 = m[k] * ms, r0 = v[k] * vs;
-            const double gd = (double)g[k];
-            m[k] = (float)__dadd_rn(__dmul_rn(how.beta1, (double)m0), __dmul_rn(1.0 - how.beta1, gd));
-            v[k] = (float)__dadd_rn(__dmul_rn(how.beta2, (double)(r0 * r0)), __dmul_rn(__dmul_rn(1.0 - how.beta2, gd), gd));
-        } else {
-            m[k] = fmaf(b1, m[k], c1 * g[k]);
-            v[k] = fmaf(b2, v[k], c2 * g[k] * g[k]);
-        }
-        const float root = __fsqrt_rn(v[k]);
-        const float update = __fdividef(m[k], fmaf(root, f.root_scale, how.eps)) * f.step_size;
-        p[k] = fmaf(-f.lr * t.weight_decay, p[k], p[k]) - update;
-        if (EIGHT) {
-            v[k] = root;
-            if (fabsf(m[k]) <= 3.4028235e38f)
-                m_max = fmaxf(m_max, fabsf(m[k]));
-            if (root <= 3.4028235e38f)
-                r_max = fmaxf(r_max, root);
-        }
+    for (int k = 0; k < 8; k += 2) {
+        const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
+        const F2 m2 = fma_f2(b1, f2(m[k], m[k + 1]), mul_f2(c1, gg));
+        const F2 v2 = fma_f2(b2, f2(v[k], v[k + 1]), mul_f2(mul_f2(c2, gg), gg));
+        put2(m, k, m2);
+        put2(v, k, v2);
+        put2(p, k, stepped(f2(p[k], p[k + 1]), m2, f2(root_of(v[k]), root_of(v[k + 1])), how, f, decay));
     }
     if (t.master)
         store8<VEC>(t.master, PEAGLE_F32, i, left, p);
     store8<VEC>(t.param, t.param_dtype, i, left, p);
-    if (!EIGHT) {
-        store8<VEC>(t.m, PEAGLE_F32, i, left, m);
-        store8<VEC>(t.v, PEAGLE_F32, i, left, v);
-        return;
+    store8<VEC>(t.m, PEAGLE_F32, i, left, m);
+    store8<VEC>(t.v, PEAGLE_F32, i, left, v);
+}
+
+// The new m and root of one element in fp64, rounded once each.
+__device__ __forceinline__ void exact_states(const How &how, float m0, float r0, float g, float &m, float &root)
+{
+    const double gd = (double)g;
+    m = (float)__dadd_rn(__dmul_rn(how.beta1, (double)m0), __dmul_rn(1.0 - how.beta1, gd));
+    root = __fsqrt_rn((float)__dadd_rn(__dmul_rn(how.beta2, (double)(r0 * r0)), __dmul_rn(__dmul_rn(1.0 - how.beta2, gd), gd)));
+}
+
+// Largest magnitudes of a doubtful block, without the elements that are not finite.  From memory: the numbers that the
+// caller has are not kept for this rare case.
+__device__ __forceinline__ void exact_largest(const Tensor &t, const How &how, float grad_scale, int64_t i, int left,
+                                              uint32_t &largest_m, uint32_t &largest_r)
+{
+    const float ms = t.m_scale[i / AW_BLOCK], vs = t.v_scale[i / AW_BLOCK];
+    uint32_t lm = 0, lr = 0;
+#pragma unroll 1
+    for (int k = 0; k < left; ++k) {
+        float m[8], r[8], g = t.grad_dtype == PEAGLE_F32 ? static_cast<const float *>(t.grad)[i + k]
+                                                         : __bfloat162float(static_cast<const __nv_bfloat16 *>(t.grad)[i + k]);
+        decode4(static_cast<const uint8_t *>(t.m)[i + k], m, 0);
+        decode4(static_cast<const uint8_t *>(t.v)[i + k], r, 0);
+        exact_states(how, m[0] * ms, r[0] * vs, g * grad_scale, m[0], r[0]);
+        const uint32_t mb = __float_as_uint(fabsf(m[0])), rb = __float_as_uint(fabsf(r[0]));
+        lm = mb < 0x7f800000u ? max(lm, mb) : lm;
+        lr = rb < 0x7f800000u ? max(lr, rb) : lr;
     }
-    const float2 sm = scale_of(warp_max(m_max)), sv = scale_of(warp_max(r_max));
-    uint32_t key = mix(f.key ^ (ordinal + 1u));
-    if (i >> 32)
-        key = mix(key ^ (uint32_t)(i >> 32));
+    largest_m = __reduce_max_sync(~0u, lm);
+    largest_r = __reduce_max_sync(~0u, lr);
+}
+
+// One thread's 8 elements of a tensor with states in 8 bits.  The whole warp, with a block of PEAGLE_ADAMW_BLOCK
+// elements; elements that are not there are zeros.
+template <bool VEC>
+__device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, const Factors &f, float grad_scale, uint32_t key,
+                                            int64_t i, int left)
+{
+    float g[8], m[8], r[8], p[8];
+    const int64_t block = i / AW_BLOCK;
+    const uint2 mc = load_codes<VEC>(t.m, i, left), vc = load_codes<VEC>(t.v, i, left);
+    const float ms = t.m_scale[block], vs = t.v_scale[block];
+    load8<VEC>(t.grad, t.grad_dtype, i, left, g);
+    load8<VEC>(t.master ? t.master : t.param, t.master ? PEAGLE_F32 : t.param_dtype, i, left, p);
+    decode4(mc.x, m, 0);
+    decode4(mc.y, m, 4);
+    decode4(vc.x, r, 0);
+    decode4(vc.y, r, 4);
+    const float decay = -f.lr * t.weight_decay, b1s = (float)how.beta1 * ms; // by a power of two: exact
+    const F2 b1 = f2(b1s, b1s), c1 = both(1.0 - how.beta1), b2 = both(how.beta2), c2 = both(1.0 - how.beta2), vs2 = f2(vs, vs);
+    float m_max = 0.f, r_max = 0.f, m_min = 1e38f, r_min = 1e38f;
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const uint32_t bits = mix(key + (uint32_t)(i + k) * GOLDEN);
-        m[k] = to_e4m3(m[k] * sm.y, bits & 0xffffu, false);
-        v[k] = to_e4m3(v[k] * sv.y, bits >> 16, v[k] > 0.f);
+    for (int k = 0; k < 8; k += 2) {
+        const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
+        const F2 m2 = fma_f2(b1, f2(m[k], m[k + 1]), mul_f2(c1, gg));
+        const F2 r0 = mul_f2(f2(r[k], r[k + 1]), vs2);
+        const float2 v = unf2(fma_f2(b2, mul_f2(r0, r0), mul_f2(mul_f2(c2, gg), gg)));
+        put2(m, k, m2);
+        r[k] = root_of(v.x);
+        r[k + 1] = root_of(v.y);
+        put2(p, k, stepped(f2(p[k], p[k + 1]), m2, f2(r[k], r[k + 1]), how, f, decay));
+        m_max = max_nan(max_nan(m_max, fabsf(m[k])), fabsf(m[k + 1]));
+        r_max = max_nan(max_nan(r_max, r[k]), r[k + 1]);
+        m_min = fminf(fminf(m_min, fabsf(m[k])), fabsf(m[k + 1]));
+        r_min = fminf(fminf(r_min, r[k]), r[k + 1]);
+    }
+    if (t.master)
+        store8<VEC>(t.master, PEAGLE_F32, i, left, p);
+    store8<VEC>(t.param, t.param_dtype, i, left, p);
+    uint32_t largest_m = __reduce_max_sync(~0u, __float_as_uint(m_max) & 0x7fffffffu);
+    uint32_t largest_r = __reduce_max_sync(~0u, __float_as_uint(r_max) & 0x7fffffffu);
+    bool finite = true;
+    if (doubtful(largest_m) || doubtful(largest_r)) {
+        finite = largest_m < 0x7f800000u && largest_r < 0x7f800000u;
+        exact_largest(t, how, grad_scale, i, left, largest_m, largest_r);
+    }
+    const float2 sm = scale_of(__uint_as_float(largest_m)), sv = scale_of(__uint_as_float(largest_r));
+    const uint32_t first = key + (uint32_t)i * GOLDEN;
+    if (finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f) {
+        const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
+#pragma unroll
+        for (int k = 0; k < 8; k += 2) {
+            const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
+            const uint32_t x = mix(first + k * GOLDEN), y = mix(first + (k + 1) * GOLDEN);
+            // the sign stays where it is: adding below it does not carry into it
+            m[k] = __uint_as_float((__float_as_uint(a.x) + bits_of_m(x)) & 0xfff00000u);
+            m[k + 1] = __uint_as_float((__float_as_uint(a.y) + bits_of_m(y)) & 0xfff00000u);
+            r[k] = __uint_as_float((__float_as_uint(b.x) + bits_of_root(x)) & 0xfff00000u);
+            r[k + 1] = __uint_as_float((__float_as_uint(b.y) + bits_of_root(y)) & 0xfff00000u);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const uint32_t bits = mix(first + k * GOLDEN);
+            const float a = fabsf(m[k]) * sm.y, b = r[k] * sv.y;
+            m[k] = a <= 256.f ? copysignf(to_e4m3(a, bits_of_m(bits)), m[k]) : __int_as_float(0x7fffffff);
+            const float root = r[k] > 0.f ? fmaxf(to_e4m3(b, bits_of_root(bits)), 0.001953125f) : 0.f; // 2^-9
+            r[k] = b <= 256.f ? root : __int_as_float(0x7fffffff);
+        }
     }
     store_codes<VEC>(t.m, i, left, make_uint2(encode4(m[0], m[1], m[2], m[3]), encode4(m[4], m[5], m[6], m[7])));
-    store_codes<VEC>(t.v, i, left, make_uint2(encode4(v[0], v[1], v[2], v[3]), encode4(v[4], v[5], v[6], v[7])));
+    store_codes<VEC>(t.v, i, left, make_uint2(encode4(r[0], r[1], r[2], r[3]), encode4(r[4], r[5], r[6], r[7])));
     if (threadIdx.x % 32 == 0) {
         t.m_scale[block] = sm.x;
         t.v_scale[block] = sv.x;
     }
 }
 
-template <int N>
-__global__ void __launch_bounds__(AW_THREADS) adamw_kernel(const __grid_constant__ Table<N> table)
+// KINDS: which states the list has, 1 in 32 bits, 2 in 8 bits (a kernel for both has the registers of the larger).
+template <int N, int KINDS>
+__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ Table<N> table)
 {
     const How &how = table.how;
     Factors f = how.factors;
@@ -334,26 +431,31 @@ __global__ void __launch_bounds__(AW_THREADS) adamw_kernel(const __grid_constant
                 hi = mid - 1;
         }
         const Tensor &t = table.t[lo];
-        const int64_t i = (int64_t)(chunk - t.first) * CHUNK + threadIdx.x * 8;
-        const int64_t rest = t.count - i;
+        const int64_t begin = (int64_t)(chunk - t.first) * CHUNK;
+        uint32_t key = mix(f.key ^ (how.ordinal + lo + 1u));
+        if (begin >> 32) // a chunk does not cross 2^32
+            key = mix(key ^ (uint32_t)(begin >> 32));
+        const int64_t i = begin + threadIdx.x * 8, rest = t.count - i;
+        if (rest + (int)(threadIdx.x % 32 * 8) <= 0)
+            continue; // the whole warp
         const int left = rest >= 8 ? 8 : rest > 0 ? (int)rest : 0;
         const bool vec = t.aligned && rest >= 8;
-        if (t.m_scale) {
+        if (KINDS == 2 || (KINDS == 3 && t.m_scale)) {
             // a warp stays together, for its block's scales
             if (__all_sync(~0u, vec))
-                step8<true, true>(t, how, f, grad_scale, how.ordinal + lo, i, left);
-            else if (__any_sync(~0u, left > 0))
-                step8<false, true>(t, how, f, grad_scale, how.ordinal + lo, i, left);
+                step8_codes<true>(t, how, f, grad_scale, key, i, left);
+            else
+                step8_codes<false>(t, how, f, grad_scale, key, i, left);
         } else if (vec) {
-            step8<true, false>(t, how, f, grad_scale, how.ordinal + lo, i, left);
+            step8<true>(t, how, f, grad_scale, i, left);
         } else if (left) {
-            step8<false, false>(t, how, f, grad_scale, how.ordinal + lo, i, left);
+            step8<false>(t, how, f, grad_scale, i, left);
         }
     }
 }
 
 template <int N>
-void launch_table(const How &how, const Tensor *t, int n_sm, cudaStream_t s)
+void launch_table(const How &how, const Tensor *t, int kinds, int n_sm, cudaStream_t s)
 {
     Table<N> table;
     table.how = how;
@@ -361,7 +463,13 @@ void launch_table(const How &how, const Tensor *t, int n_sm, cudaStream_t s)
         table.t[i] = t[i];
     // a block per chunk; where each has to form the factors, no more than fit the GPU
     const uint32_t most = how.lr_dev || how.step_dev ? 4u * n_sm : how.chunks;
-    adamw_kernel<N><<<how.chunks < most ? how.chunks : most, AW_THREADS, 0, s>>>(table);
+    const uint32_t blocks = how.chunks < most ? how.chunks : most;
+    if (kinds == 1)
+        adamw_kernel<N, 1><<<blocks, AW_THREADS, 0, s>>>(table);
+    else if (kinds == 2)
+        adamw_kernel<N, 2><<<blocks, AW_THREADS, 0, s>>>(table);
+    else
+        adamw_kernel<N, 3><<<blocks, AW_THREADS, 0, s>>>(table);
 }
 
 } // namespace
@@ -387,6 +495,7 @@ int launch_adamw(const peagle_adamw_t &how, const peagle_adamw_tensor_t *tensors
         Tensor list[PEAGLE_ADAMW_TENSORS];
         h.ordinal = (uint32_t)from;
         h.chunks = 0;
+        int kinds = 0;
         for (h.n = 0; h.n < PEAGLE_ADAMW_TENSORS && from < n; ++from) {
             const peagle_adamw_tensor_t &t = tensors[from];
             Tensor &d = list[h.n++];
@@ -407,12 +516,13 @@ int launch_adamw(const peagle_adamw_t &how, const peagle_adamw_tensor_t *tensors
                           reinterpret_cast<uintptr_t>(t.master)) % 16 == 0) &&
                         states % (t.m_scale ? 8 : 16) == 0;
             h.chunks += (uint32_t)((t.count + CHUNK - 1) / CHUNK);
+            kinds |= t.count == 0 ? 0 : t.m_scale ? 2 : 1;
         }
         if (h.chunks) {
             if (h.n <= SHORT_LIST)
-                launch_table<SHORT_LIST>(h, list, n_sm, s);
+                launch_table<SHORT_LIST>(h, list, kinds, n_sm, s);
             else
-                launch_table<PEAGLE_ADAMW_TENSORS>(h, list, n_sm, s);
+                launch_table<PEAGLE_ADAMW_TENSORS>(h, list, kinds, n_sm, s);
             ++launches;
         }
     }
