@@ -9,7 +9,7 @@
 //     dx_j = scale ( g ([j = token] - p_j) - h p_j (log p_j + entropy) ).
 //
 // Bound by memory.  A block takes a row in chunks of 16 bytes per thread and load, the next chunk on its way.  Few
-// rows are cut into parts for a cluster of up to 8 blocks, which join through distributed shared memory.
+// rows are cut into parts for a cluster of up to 16 blocks, which join through distributed shared memory.
 //
 // Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
 // k-th largest of the maxima of 64 groups of threads, then the k-th best entry so far).  A chunk's maximum, which the
@@ -37,10 +37,9 @@ constexpr int GROUPS = 64;     // of threads, whose maxima give the first bound
 constexpr int STAGES = 2;     // chunks on their way or at hand
 constexpr int LIST = 1024;    // entries of the list of candidates
 constexpr int COUNTED = 512; // entries that are ranked by counting, at most
-constexpr int MAX_CLUSTER = 8;
 constexpr int LEAST_PART = 4096; // entries of a row's part
 static_assert(GROUPS >= PEAGLE_MAX_TOP_K && LP_THREADS % GROUPS == 0, "a first bound for every k");
-static_assert(MAX_CLUSTER * PEAGLE_MAX_TOP_K <= COUNTED && COUNTED <= LIST, "the lists of a cluster are ranked at once");
+static_assert(8 * PEAGLE_MAX_TOP_K <= COUNTED && COUNTED <= LIST, "the lists of a cluster fit one");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float T_FLOOR = -300.f; // below this, in powers of two, a probability is zero in fp32
 constexpr float LSE_LARGE = 8192.f; // from here on fp32 keeps less than 2^-10 of a log-sum-exp
@@ -170,6 +169,40 @@ __device__ __noinline__ uint64_t kth_best(const uint64_t *list, int n, int k)
     return bound;
 }
 
+// An entry's place is the number of better ones: EACH entries to a thread.
+template <int EACH>
+__device__ __forceinline__ void rank_list(uint64_t *list, int n, int k)
+{
+    uint64_t mine[EACH];
+    int place[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+        const int i = threadIdx.x + j * LP_THREADS;
+        mine[j] = i < n ? list[i] : 0;
+        place[j] = 0;
+    }
+    const ulonglong2 *pairs = reinterpret_cast<const ulonglong2 *>(list);
+#pragma unroll 8
+    for (int o = 0; o < n / 2; ++o) {
+        const ulonglong2 other = pairs[o];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+            place[j] += (other.x > mine[j]) + (other.y > mine[j]);
+    }
+    if (n & 1) {
+        const uint64_t other = list[n - 1];
+#pragma unroll
+        for (int j = 0; j < EACH; ++j)
+            place[j] += other > mine[j];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < EACH; ++j)
+        if (mine[j] && place[j] < k)
+            list[place[j]] = mine[j];
+    __syncthreads();
+}
+
 // Sorts a list and cuts it to its k best; an entry of 0 is none.  The whole block; a barrier before and after.
 __device__ __noinline__ void cut_list(uint64_t *list, int n, int k)
 {
@@ -189,36 +222,12 @@ __device__ __noinline__ void cut_list(uint64_t *list, int n, int k)
             list[threadIdx.x] = kept[threadIdx.x];
         __syncthreads();
     }
-    // an entry's place is the number of better ones
-    constexpr int EACH = COUNTED / LP_THREADS;
-    uint64_t mine[EACH];
-    int place[EACH];
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-        const int i = threadIdx.x + j * LP_THREADS;
-        mine[j] = i < n ? list[i] : 0;
-        place[j] = 0;
-    }
-    if (n <= LP_THREADS) {
-        if (mine[0])
-#pragma unroll 4
-            for (int o = 0; o < n; ++o)
-                place[0] += list[o] > mine[0];
-    } else {
-#pragma unroll 4
-        for (int o = 0; o < n; ++o) {
-            const uint64_t other = list[o];
-#pragma unroll
-            for (int j = 0; j < EACH; ++j)
-                place[j] += other > mine[j];
-        }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < EACH; ++j)
-        if (mine[j] && place[j] < k)
-            list[place[j]] = mine[j];
-    __syncthreads();
+    if (n <= LP_THREADS)
+        rank_list<1>(list, n, k);
+    else if (n <= 2 * LP_THREADS)
+        rank_list<2>(list, n, k);
+    else
+        rank_list<COUNTED / LP_THREADS>(list, n, k);
 }
 
 __device__ __forceinline__ uint64_t load_remote(const uint64_t *p, uint32_t rank)
@@ -312,10 +321,11 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
     constexpr int N = Piece<T>::N, U = FWD_PIECES, STEP = U * LP_THREADS;
     // a thread's pieces wait in its own places: no barrier between their arrival and their use
     extern __shared__ uint4 ring[]; // [STAGES][U][LP_THREADS]
-    __shared__ uint64_t list[TOP ? LIST : 1];
+    __shared__ __align__(16) uint64_t list[TOP ? LIST : 2];
     __shared__ int count; // entries that came to the list; those past its end have been dropped
     __shared__ float4 first_max[TOP ? GROUPS / 4 : 1];
     __shared__ float first_bound;
+    __shared__ uint64_t share_bound;
     __shared__ Sums warp_sums[LP_WARPS], sums;
     __shared__ RowStats stats;
     const int r = blockIdx.x / parts, part = blockIdx.x - r * parts;
@@ -345,6 +355,9 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
         count = 0;
     Sums s = {-INF, 0.f, 0.f};
     float bound = -INF; // an entry at or above it may be among the k best
+    // A list that has grown by half is cut.  (4,096 rows of 128,000, k = 20: 264 us; when it has tripled 275.)  A short
+    // part ends before that pays.
+    const int long_list = pieces <= 4 * STEP ? max(LP_THREADS - 8, a.top_k + a.top_k / 2) : a.top_k + a.top_k / 2 + 6;
     int stage = 0;
     for (int first = 0; first < pieces; first += STEP) {
         asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
@@ -473,7 +486,7 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                         }
                     }
                 }
-                if (!__syncthreads_or(end > k + k / 2 + 6)) {
+                if (!__syncthreads_or(end > long_list)) {
                     if (first == 0)
                         bound = from_key(order_key(bound) + 1); // k entries of this chunk, with lower ids, reach it
                     break;
@@ -534,9 +547,14 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
     if (parts > 1) {
         cluster_sync_all();
         if (part == 0) {
-            if (threadIdx.x == 0)
-                for (int p = 1; p < parts; ++p)
-                    s = join(s, {load_remote(&sums.m, p), load_remote(&sums.S, p), load_remote(&sums.E, p)}, l);
+            if (threadIdx.x < 32) {
+                const int p = threadIdx.x % parts; // a power of two
+                s = {load_remote(&sums.m, p), load_remote(&sums.S, p), load_remote(&sums.E, p)};
+                for (int o = 1; o < parts; o *= 2) {
+                    const Sums other = {__shfl_xor_sync(~0u, s.m, o), __shfl_xor_sync(~0u, s.S, o), __shfl_xor_sync(~0u, s.E, o)};
+                    s = join(s, other, l);
+                }
+            }
             if (TOP) {
                 const int k = a.top_k;
                 uint64_t theirs[COUNTED / LP_THREADS];
@@ -545,12 +563,26 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                     const int i = threadIdx.x + j * LP_THREADS;
                     theirs[j] = i < parts * k ? load_remote(&list[i % k], i / k) : 0;
                 }
+                // what is below the part's share of k in every part is not among the k best
+                const int share = (k - 1) / parts;
+                uint64_t least = threadIdx.x < parts ? load_remote(&list[share], threadIdx.x) : ~0ull;
+                for (int o = 8; o; o >>= 1) {
+                    const uint64_t other = __shfl_xor_sync(~0u, least, o);
+                    least = other < least ? other : least;
+                }
+                __syncthreads(); // the first part's own list has been read
+                if (threadIdx.x == 0) {
+                    share_bound = least;
+                    count = 0;
+                }
                 __syncthreads();
+                least = share_bound;
 #pragma unroll
                 for (int j = 0; j < COUNTED / LP_THREADS; ++j)
-                    list[threadIdx.x + j * LP_THREADS] = theirs[j];
+                    if (theirs[j] && theirs[j] >= least)
+                        list[atomicAdd(&count, 1)] = theirs[j];
                 __syncthreads();
-                cut_list(list, parts * k, k);
+                cut_list(list, count, k);
             }
         }
         cluster_sync_all(); // nobody leaves while its lists are read
@@ -684,8 +716,13 @@ void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
     const auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
     // few rows are cut as long as the GPU has places left
     int parts = 1;
-    while (parts < MAX_CLUSTER && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
+    while (parts < 8 && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
         parts *= 2;
+    // clusters of 16 are harder to place: 16 rows of 128,000 take 20.7 us with them and 14.4 without, one 13.3 and 13.4
+    if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED)
+        parts = 16;
+    if (parts > 8)
+        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     const int part_len = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
