@@ -716,7 +716,7 @@ void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
     const auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
     // few rows are cut as long as the GPU has places left
     int parts = 1;
-    while (parts < 8 && (int64_t)a.rows * parts * 2 <= 4 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
+    while (parts < 8 && (int64_t)a.rows * parts * 2 <= 8 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
         parts *= 2;
     // clusters of 16 are harder to place: 16 rows of 128,000 take 20.7 us with them and 14.4 without, one 13.3 and 13.4
     if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED)

@@ -15,6 +15,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "peagle_internal.h"
 #include "sm100_ptx.cuh"
@@ -48,11 +49,15 @@ __host__ __device__ constexpr int block_threads(int tpr) { return tpr == 192 ? 3
 
 // What thread t of a group has of a row: E elements, in 16-byte pieces TPR pieces apart (VEC: base addresses and
 // row strides are multiples of 16 bytes), or single elements TPR apart.
-template <class T, bool VEC, int TPR, int E>
+// FP32_AHEAD: single fp32 elements are fetched ahead too, 4 bytes at a time, which pays in the forward (16,384 rows of
+// 2,877: 99 -> 80 us) and not in the backward with its two tensors (30,000 rows of 1,001: 66 -> 84).
+template <class T, bool VEC, int TPR, int E, bool FP32_AHEAD = false>
 struct Part {
     static constexpr int PIECE = VEC ? 16 / (int)sizeof(T) : 1;
     static constexpr int N = E / PIECE;
     static constexpr bool PACKED = VEC && sizeof(T) == 2; // bf16 pairs stay packed
+    static constexpr bool AHEAD = VEC || (sizeof(T) == 4 && FP32_AHEAD);
+    using Slot = std::conditional_t<VEC, uint4, uint32_t>;
     static constexpr int WORDS = PACKED ? E / 2 : E;
     uint32_t raw[WORDS];
 
@@ -64,30 +69,33 @@ struct Part {
         return ((e / Q) * TPR + t) * Q + e % Q;
     }
 
-    // Starts to fetch the share of a row, into the thread's own places in `stage` (shared memory, 16 bytes x threads
-    // for every piece); single elements are fetched when they are taken.  `row` is the row's address plus t pieces.
+    // Starts to fetch the share of a row, into the thread's own places in `stage` (shared memory, a slot x threads
+    // for every piece); single bf16 elements are fetched when they are taken.  `row` is the row's address plus t pieces.
     static __device__ __forceinline__ void fetch(const T *row, int t, int cols, uint32_t stage)
     {
-        if constexpr (VEC) {
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int n = 0; n < N; ++n)
-                if ((n * TPR + t) * PIECE < cols)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(stage + n * block_threads(TPR) * 16),
-                                 "l"(row + n * TPR * PIECE)
-                                 : "memory");
+                if ((n * TPR + t) * PIECE < cols) {
+                    const uint32_t to = stage + n * block_threads(TPR) * (uint32_t)sizeof(Slot);
+                    if constexpr (VEC)
+                        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(row + n * TPR * PIECE) : "memory");
+                    else
+                        asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(to), "l"(row + n * TPR) : "memory");
+                }
         }
     }
     // Places past the last column are never fetched: zeros, once.
-    static __device__ __forceinline__ void clear(int t, int cols, uint4 *stage)
+    static __device__ __forceinline__ void clear(int t, int cols, Slot *stage)
     {
-        if constexpr (VEC) {
+        if constexpr (AHEAD) {
 #pragma unroll
             for (int n = 0; n < N; ++n)
                 if ((n * TPR + t) * PIECE >= cols)
-                    stage[n * block_threads(TPR)] = make_uint4(0, 0, 0, 0);
+                    stage[n * block_threads(TPR)] = Slot{};
         }
     }
-    __device__ __forceinline__ void take(const T *row, int t, int cols, const uint4 *stage)
+    __device__ __forceinline__ void take(const T *row, int t, int cols, const Slot *stage)
     {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -97,6 +105,8 @@ struct Part {
                 raw[4 * n + 1] = v.y;
                 raw[4 * n + 2] = v.z;
                 raw[4 * n + 3] = v.w;
+            } else if constexpr (AHEAD) {
+                raw[n] = stage[n * block_threads(TPR)];
             } else {
                 raw[n] = n * TPR + t < cols ? __float_as_uint(load1(row + n * TPR)) : 0u;
             }
@@ -164,9 +174,10 @@ struct Part {
 // the widest groups' 227 KB, fp32 weights and bias take 128).
 template <class T, bool VEC, int TPR, int E, int TENSORS>
 struct Ring {
-    static constexpr int PIECES = VEC ? TENSORS * E * (int)sizeof(T) / 16 : 0;
-    static constexpr int DEPTH = !VEC || (TPR == 1024 && sizeof(T) == 4) ? 1 : 2;
-    static constexpr int BYTES = DEPTH * PIECES * 16; // per thread
+    using Row = Part<T, VEC, TPR, E, TENSORS == 1>;
+    static constexpr int SLOTS = Row::AHEAD ? TENSORS * Row::N : 0;
+    static constexpr int DEPTH = !Row::AHEAD || (TPR == 1024 && sizeof(T) == 4) ? 1 : 2;
+    static constexpr int BYTES = DEPTH * SLOTS * (int)sizeof(typename Row::Slot); // per thread
 };
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int LEFT>
@@ -250,12 +261,13 @@ constexpr int fwd_blocks(bool layer, int words, int tpr, int threads)
 template <class T, bool VEC, int TPR, int E>
 __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __grid_constant__ NormArgs a)
 {
-    using Row = Part<T, VEC, TPR, E>;
     using Stages = Ring<T, VEC, TPR, E, 1>;
-    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::PIECES * BT;
+    using Row = typename Stages::Row;
+    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::SLOTS * BT;
     extern __shared__ float4 smem[];
-    uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
-    float *sw = reinterpret_cast<float *>(smem + D * STAGE), *sb = sw + TPR * E;
+    constexpr int SLOT = sizeof(typename Row::Slot);
+    auto *ring = reinterpret_cast<typename Row::Slot *>(smem) + threadIdx.x;
+    float *sw = reinterpret_cast<float *>(reinterpret_cast<char *>(smem) + Stages::BYTES * BT), *sb = sw + TPR * E;
     __shared__ float red1[2][BT / 32];
     __shared__ __align__(16) float2 red2[2][BT / 32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
@@ -269,7 +281,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
     for (int i = 0; i < D; ++i) {
         Row::clear(t, cols, ring + i * STAGE);
         if (first + i * step < rows)
-            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * 16);
+            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * SLOT);
         copies_commit();
     }
     stage_weights<Row, E, G>(sw, a.weight, a.w_dtype, 1.f, t, g, cols);
@@ -321,7 +333,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
         }
         // the sums are formed, so the stage has been read
         if (r + D * step < rows)
-            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * 16);
+            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * SLOT);
         copies_commit();
         if (D > 1)
             stage ^= 1;
@@ -371,12 +383,13 @@ __global__ void __launch_bounds__(block_threads(TPR),
                                   blocks_per_sm(block_threads(TPR), 2 * Part<T, VEC, TPR, E>::WORDS + SUMS * E))
     norm_bwd_kernel(const __grid_constant__ NormArgs a)
 {
-    using Row = Part<T, VEC, TPR, E>;
     using Stages = Ring<T, VEC, TPR, E, 2>;
-    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::PIECES * BT, HALF = STAGE / 2;
+    using Row = typename Stages::Row;
+    constexpr int BT = block_threads(TPR), G = BT / TPR, D = Stages::DEPTH, STAGE = Stages::SLOTS * BT, HALF = STAGE / 2;
     extern __shared__ float4 smem[];
-    uint4 *ring = reinterpret_cast<uint4 *>(smem) + threadIdx.x;
-    float *sw = reinterpret_cast<float *>(smem + D * STAGE);
+    constexpr int SLOT = sizeof(typename Row::Slot);
+    auto *ring = reinterpret_cast<typename Row::Slot *>(smem) + threadIdx.x;
+    float *sw = reinterpret_cast<float *>(reinterpret_cast<char *>(smem) + Stages::BYTES * BT);
     __shared__ float red1[2][BT / 32];
     __shared__ __align__(16) float2 red[2][BT / 32];
     const int t = threadIdx.x % TPR, g = threadIdx.x / TPR, cols = a.cols;
@@ -391,8 +404,8 @@ __global__ void __launch_bounds__(block_threads(TPR),
         Row::clear(t, cols, ring + i * STAGE);
         Row::clear(t, cols, ring + i * STAGE + HALF);
         if (first + i * step < rows) {
-            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * 16);
-            Row::fetch(dy_at(first + i * step), t, cols, ring_at + (i * STAGE + HALF) * 16);
+            Row::fetch(x_at(first + i * step), t, cols, ring_at + i * STAGE * SLOT);
+            Row::fetch(dy_at(first + i * step), t, cols, ring_at + (i * STAGE + HALF) * SLOT);
         }
         copies_commit();
     }
@@ -453,8 +466,8 @@ __global__ void __launch_bounds__(block_threads(TPR),
             s = make_float2(0.f, group_sum<TPR>(p1.x + p1.y, red1, turn));
         // the sums are formed, so the stage has been read
         if (r + D * step < rows) {
-            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * 16);
-            Row::fetch(dy_at(r + D * step), t, cols, ring_at + (stage * STAGE + HALF) * 16);
+            Row::fetch(x_at(r + D * step), t, cols, ring_at + stage * STAGE * SLOT);
+            Row::fetch(dy_at(r + D * step), t, cols, ring_at + (stage * STAGE + HALF) * SLOT);
         }
         copies_commit();
         if (D > 1)
