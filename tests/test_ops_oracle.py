@@ -287,3 +287,28 @@ def test_adamw_refuses_bad_lists(lib, zeros):
     assert lib.peagle_adamw_step(zeros, None, None, 0, None) == S["NULL"]
     how = binding.peagle_adamw_t(1e-3, 0.9, 0.99, 1e-8, 1)
     assert lib.peagle_adamw_step(zeros, ctypes.byref(how), None, 2, None) == S["NULL"]
+
+
+# ------------------------------------------------------------------ the binding's own checks, on host tensors
+class _Context:
+    """Device 0 and no handle: a call that came to the library would be refused as NULL."""
+    h, device = None, 0
+
+
+def test_binding_refuses_host_tensors(lib):
+    from paper_2602_01469_b200 import binding as b
+    b._know_torch()
+    x, f, i = torch.zeros(3, 8), torch.zeros(3), torch.zeros(3, dtype=torch.int32)
+    calls = [
+        lambda: b.peagle_norm_fwd(_Context, 0, x, None, None, 1e-5, x),
+        lambda: b.peagle_norm_fwd(_Context, 0, x[0], None, None, 1e-5, x[0]),
+        lambda: b.peagle_norm_bwd(_Context, 1, x, None, None, f, x, x),
+        lambda: b.peagle_token_logprobs_fwd(_Context, x, i, 1.0, f),
+        lambda: b.peagle_token_logprobs_fwd(_Context, x, None, 1.0, None, None, None, x, None),
+        lambda: b.peagle_token_logprobs_bwd(_Context, x, i, 1.0, f, None, f, None, x),
+        lambda: b.AdamWTensors([{"param": x, "grad": x, "m": x, "v": x}]),
+    ]
+    for call in calls:
+        with pytest.raises(b.PeagleError) as e:
+            call()
+        assert e.value.status == b.STATUS["BAD_SHAPE"]
