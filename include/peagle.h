@@ -320,7 +320,7 @@ typedef enum peagle_dtype { PEAGLE_F32 = 0, PEAGLE_BF16 = 1 } peagle_dtype;
  *     rstd = 1 / sqrt(mean((x - mu)^2) + eps),   y = (x - mu) * rstd * weight + bias
  * X, Y are dev [rows][cols] of x_dtype; weight, bias dev [cols] of w_dtype, each may be NULL (1 and 0).
  * mean, rstd are dev fp32 [rows], what the backward needs; each may be NULL (mean is not written by
- * PEAGLE_NORM_RMS).  eps > 0.  In place: Y may be X with the same leading dimension.  A NaN or infinity
+ * PEAGLE_NORM_RMS).  eps > 0, cols <= 2^30 (up to 16,384 a row is read once).  In place: Y may be X with the same leading dimension.  A NaN or infinity
  * stays in its row.  Asynchronous.
  */
 typedef enum peagle_norm { PEAGLE_NORM_LAYER = 0, PEAGLE_NORM_RMS = 1 } peagle_norm;
@@ -345,7 +345,7 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
 /*
  * Log probabilities of given tokens, with entropy and top alternatives: the loss on the drafted tokens
  * (Section 2: the drafter predicts K tokens at once), or the scores of a served request.  With
- * s_j = scale * logits[r][j] (0 < scale <= 1e20, an inverse temperature):
+ * s_j = scale * logits[r][j] (an inverse temperature, 1e-20 to 1e20):
  *     lse = log sum_j exp(s_j),  logprob = s_token - lse,  entropy = -sum_j p_j log p_j,  p_j = exp(s_j - lse)
  * and, of the top_k largest logits, top_ids (larger logit first, of equal ones the lower id first; -0 equals
  * 0) and top_logprobs = s_id - lse.  logits is dev [rows][vocab] of `dtype`; tokens dev int32 [rows], -1

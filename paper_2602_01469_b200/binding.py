@@ -192,9 +192,9 @@ def _matrix(t, rows, cols, dtype, device):
     if t.shape != (rows, cols) or t.dtype != dtype or t.get_device() != device:
         _refuse()
     ld, inner = t.stride()
-    if inner != 1 and cols > 1:
+    if inner != 1 and cols > 1 and rows:
         _refuse()
-    return t.data_ptr(), ld if rows != 1 else max(ld, cols)
+    return t.data_ptr(), ld if rows > 1 else max(ld, cols)
 
 
 def _vector(t, n, dtypes, device):

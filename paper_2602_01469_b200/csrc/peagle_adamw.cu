@@ -13,11 +13,11 @@
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, about 70 per element and half of them integer ones for the random bits and the
-// roundings, and the wait for memory with registers for no more than four blocks.  The first version had 113: it
-// formed the new m and v in fp64 so that the codes would not depend on how the arithmetic is ordered.  In fp32 two or
-// three codes in a million fall on the other side of the random bits, which is as good a rounding; only a block's
-// scale has to be right, and where a block's largest number lies at a power of two, or is not finite, the largest is
-// found again in fp64.
+// roundings: 91 M elements, bf16, take 238 us, 59 % of the copy rate.  A first version had 113 and took 343; it formed
+// the new m and v in fp64 so that the codes would not depend on how the arithmetic is ordered.  In fp32 two or three
+// codes in a million fall on the other side of the random bits, which is as good a rounding; only a block's scale has
+// to be right, and where a block's largest number lies at a power of two, or is not finite, the largest is found
+// again in fp64.  (Blocks that stay, with the next chunk on its way in shared memory, have more instructions: 260.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -33,8 +33,8 @@ namespace {
 
 constexpr int AW_THREADS = 256;
 constexpr int AW_BLOCK = PEAGLE_ADAMW_BLOCK;
-// Elements per thread block, 8 per thread.  (Blocks that go on to a second and third 2,048 spend fewer instructions on
-// finding their tensor and wait longer for memory: 8-bit states of 91 M elements 254 us, with two 300, with four 283.)
+// Elements per thread block, 8 per thread.  (Blocks that go on to a second 2,048 spend fewer instructions on finding
+// their tensor and wait longer for memory: 8-bit states of 91 M elements 300 instead of 254 us, with four blocks to an SM.)
 constexpr int CHUNK = (AW_THREADS / 32) * AW_BLOCK;
 constexpr uint32_t GOLDEN = 0x9E3779B9u;            // 2^32 / golden ratio
 
@@ -205,11 +205,15 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
     return (uint32_t)hi << 16 | lo;
 }
 
-// y >= 0 rounded up or down to an e4m3 number: `bits20` are 20 random bits.
-__device__ __forceinline__ float to_e4m3(float y, uint32_t bits20)
+// y rounded up or down by 20 random bits, where the plain way (`large`) does not do: below 2^-6, where e4m3's spacing is
+// even, and not finite.  `keep`: above zero stays above it.
+__device__ __forceinline__ float small_code(float y, float large, uint32_t bits20, bool keep)
 {
-    const float shift = y < 0.015625f ? 0.015625f : 0.f;
-    return __uint_as_float((__float_as_uint(y + shift) + bits20) & 0xfff00000u) - shift;
+    const float a = fabsf(y);
+    if (a >= 0.015625f)
+        return a <= 256.f ? large : __int_as_float(0x7fffffff);
+    const float z = __uint_as_float((__float_as_uint(a + 0.015625f) + bits20) & 0xfff00000u) - 0.015625f;
+    return a != a ? a : copysignf(keep && a > 0.f ? fmaxf(z, 0.001953125f) : z, y); // 2^-9
 }
 // The 20 bits of an element's random 32 for m and for the root: 16 of them and a half.
 __device__ __forceinline__ uint32_t bits_of_m(uint32_t bits) { return (bits << 4 & 0xffff0u) | 8u; }
@@ -377,26 +381,22 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     }
     const float2 sm = scale_of(__uint_as_float(largest_m)), sv = scale_of(__uint_as_float(largest_r));
     const uint32_t first = key + (uint32_t)i * GOLDEN;
-    if (finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f) {
-        const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
+    const bool plain = finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f;
+    const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
 #pragma unroll
-        for (int k = 0; k < 8; k += 2) {
-            const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
-            const uint32_t x = mix(first + k * GOLDEN), y = mix(first + (k + 1) * GOLDEN);
-            // the sign stays where it is: adding below it does not carry into it
-            m[k] = __uint_as_float((__float_as_uint(a.x) + bits_of_m(x)) & 0xfff00000u);
-            m[k + 1] = __uint_as_float((__float_as_uint(a.y) + bits_of_m(y)) & 0xfff00000u);
-            r[k] = __uint_as_float((__float_as_uint(b.x) + bits_of_root(x)) & 0xfff00000u);
-            r[k + 1] = __uint_as_float((__float_as_uint(b.y) + bits_of_root(y)) & 0xfff00000u);
-        }
-    } else {
-#pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const uint32_t bits = mix(first + k * GOLDEN);
-            const float a = fabsf(m[k]) * sm.y, b = r[k] * sv.y;
-            m[k] = a <= 256.f ? copysignf(to_e4m3(a, bits_of_m(bits)), m[k]) : __int_as_float(0x7fffffff);
-            const float root = r[k] > 0.f ? fmaxf(to_e4m3(b, bits_of_root(bits)), 0.001953125f) : 0.f; // 2^-9
-            r[k] = b <= 256.f ? root : __int_as_float(0x7fffffff);
+    for (int k = 0; k < 8; k += 2) {
+        const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
+        const uint32_t x = mix(first + k * GOLDEN), y = mix(first + (k + 1) * GOLDEN);
+        // the sign stays where it is: adding below it does not carry into it
+        m[k] = __uint_as_float((__float_as_uint(a.x) + bits_of_m(x)) & 0xfff00000u);
+        m[k + 1] = __uint_as_float((__float_as_uint(a.y) + bits_of_m(y)) & 0xfff00000u);
+        r[k] = __uint_as_float((__float_as_uint(b.x) + bits_of_root(x)) & 0xfff00000u);
+        r[k + 1] = __uint_as_float((__float_as_uint(b.y) + bits_of_root(y)) & 0xfff00000u);
+        if (!plain) { // small numbers, roots that must not become zero, and what is not finite
+            m[k] = small_code(a.x, m[k], bits_of_m(x), false);
+            m[k + 1] = small_code(a.y, m[k + 1], bits_of_m(y), false);
+            r[k] = small_code(b.x, r[k], bits_of_root(x), true);
+            r[k + 1] = small_code(b.y, r[k + 1], bits_of_root(y), true);
         }
     }
     store_codes<VEC>(t.m, i, left, make_uint2(encode4(m[0], m[1], m[2], m[3]), encode4(m[4], m[5], m[6], m[7])));
@@ -407,9 +407,10 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     }
 }
 
-// KINDS: which states the list has, 1 in 32 bits, 2 in 8 bits (a kernel for both has the registers of the larger).
+// KINDS: which states the list has, 1 in 32 bits, 2 in 8 bits, 3 both (with the registers of the larger).  8-bit states
+// alone are best with five blocks to an SM and 48 registers: 238 us, with four 251, with six, which spill, 262.
 template <int N, int KINDS>
-__global__ void __launch_bounds__(AW_THREADS, 4) adamw_kernel(const __grid_constant__ Table<N> table)
+__global__ void __launch_bounds__(AW_THREADS, KINDS == 2 ? 5 : 4) adamw_kernel(const __grid_constant__ Table<N> table)
 {
     const How &how = table.how;
     Factors f = how.factors;

@@ -1259,7 +1259,7 @@ static int norm_args_ok(const NormArgs &a)
     if ((a.kind != PEAGLE_NORM_LAYER && a.kind != PEAGLE_NORM_RMS) || !dtype_size(a.x_dtype) ||
         !dtype_size(a.w_dtype) || a.rows < 0 || a.cols < 1)
         return PEAGLE_ERR_BAD_SHAPE;
-    return PEAGLE_OK;
+    return a.cols > 1 << 30 ? PEAGLE_ERR_TOO_LARGE : PEAGLE_OK;
 }
 
 int peagle_norm_fwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
@@ -1356,7 +1356,7 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
 
 static int logprob_args_ok(int32_t dtype, int32_t rows, int32_t vocab, int64_t ld, float scale)
 {
-    if (!dtype_size(dtype) || rows < 0 || vocab < 1 || ld < vocab || !(scale > 0.f && scale <= 1e20f))
+    if (!dtype_size(dtype) || rows < 0 || vocab < 1 || ld < vocab || !(scale >= 1e-20f && scale <= 1e20f))
         return PEAGLE_ERR_BAD_SHAPE;
     return vocab > 1 << 30 ? PEAGLE_ERR_TOO_LARGE : PEAGLE_OK;
 }

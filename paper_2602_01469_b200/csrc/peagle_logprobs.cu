@@ -1,6 +1,6 @@
 // Log probabilities of given tokens, entropy and top alternatives of rows of logits, and the gradient.
 //
-// Forward: one read of the logits.  In powers of two, with l = scale log2(e), m the maximum and c = m l rounded:
+// Forward: one read of the logits.  In powers of two, with l = scale log2(e), m the maximum and c = m l rounded up:
 //     t_j = x_j l - c,  S = sum 2^t_j,  E = sum 2^t_j t_j,  log S = ln 2 (log2 S - (m l - c))
 //     lse = scale m + log S,  logprob = scale (x_token - m) - log S,  entropy = ln 2 (log2 S - E / S)
 // where x l - c and m l - c are fused operations: logprob and entropy do not lose the digits that a large m would
@@ -20,6 +20,7 @@
 #include <cuda_bf16.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "peagle_internal.h"
 #include "sm100_ptx.cuh"
@@ -42,6 +43,7 @@ static_assert(GROUPS >= PEAGLE_MAX_TOP_K && LP_THREADS % GROUPS == 0, "a first b
 static_assert(8 * PEAGLE_MAX_TOP_K <= COUNTED && COUNTED <= LIST, "the lists of a cluster fit one");
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float T_FLOOR = -300.f; // below this, in powers of two, a probability is zero in fp32
+constexpr float REFERENCE_LARGE = 65536.f; // from here on, in powers of two, x l - c has lost digits
 constexpr float LSE_LARGE = 8192.f; // from here on fp32 keeps less than 2^-10 of a log-sum-exp
 constexpr float INF = __builtin_huge_valf();
 
@@ -84,11 +86,12 @@ struct Sums {
     float m, S, E; // E in powers of two
 };
 
-// What S and E refer to.  Without a maximum S is 0 (or NaN), whatever they refer to.  The bounds keep it a number
-// where m l is none, so that rescaling such a sum by 2^-huge leaves 0 and not NaN.
+// What S and E refer to: m l rounded up, so that no t is above zero, however coarse the numbers near m l are (entries
+// masked with -1e30: a thread that has seen nothing else would have a sum of 2^huge, and then infinity times zero).
+// Without a maximum S is 0 (or NaN), whatever it refers to.
 __device__ __forceinline__ float reference(float m, float l)
 {
-    return m == -INF ? 0.f : fminf(fmaxf(m * l, -3.4028235e38f), 3.4028235e38f);
+    return m == -INF ? 0.f : fminf(fmaxf(__fmul_ru(m, l), -3.4028235e38f), 3.4028235e38f);
 }
 
 __device__ __forceinline__ void rescale(Sums &s, float m, float l)
@@ -598,8 +601,8 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
     }
     __syncthreads();
     s = sums;
-    if (fabsf(s.m) < INF && fabsf(s.m * l) == INF) {
-        // m is a number and m l is not (a row of the type's lowest): again, with x - m in the place of x
+    if (fabsf(s.m) < INF && fabsf(s.m * l) >= REFERENCE_LARGE) {
+        // a row of numbers far from zero, masked throughout for one: again, with x - m in the place of x
         const float m = s.m;
         float S = 0.f, E = 0.f;
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
@@ -710,6 +713,38 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
     }
 }
 
+constexpr int FWD_SMEM = STAGES * FWD_PIECES * LP_THREADS * 16;
+
+// Whether the GPU places clusters of 16 blocks of a kernel, more than every GPU has to.  Asked once per kernel (all
+// devices here are alike).
+template <class Kernel>
+bool takes_16(Kernel kernel)
+{
+    static std::atomic<int> known; // 0 not asked, 1 no, 2 yes
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    if (known.load(std::memory_order_relaxed) == 0) {
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute at[1];
+        at[0].id = cudaLaunchAttributeClusterDimension;
+        at[0].val.clusterDim.x = 16;
+        at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3(16);
+        cfg.blockDim = dim3(LP_THREADS);
+        cfg.dynamicSmemBytes = FWD_SMEM;
+        cfg.attrs = at;
+        cfg.numAttrs = 1;
+        int n = 0;
+        const bool yes = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
+        if (!yes)
+            cudaGetLastError();
+        known.store(yes ? 2 : 1, std::memory_order_relaxed);
+    }
+    return known.load(std::memory_order_relaxed) == 2;
+}
+
 template <class T, bool ENTROPY, bool TOP>
 void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
 {
@@ -719,10 +754,8 @@ void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
     while (parts < 8 && (int64_t)a.rows * parts * 2 <= 8 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
         parts *= 2;
     // clusters of 16 are harder to place: 16 rows of 128,000 take 20.7 us with them and 14.4 without, one 13.3 and 13.4
-    if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED)
+    if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED && takes_16(kernel))
         parts = 16;
-    if (parts > 8)
-        cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     const int part_len = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute at[1];
@@ -731,7 +764,7 @@ void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
     at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
     cfg.gridDim = dim3((unsigned)a.rows * parts);
     cfg.blockDim = dim3(LP_THREADS);
-    cfg.dynamicSmemBytes = STAGES * FWD_PIECES * LP_THREADS * 16;
+    cfg.dynamicSmemBytes = FWD_SMEM;
     cfg.stream = s;
     cfg.attrs = at;
     cfg.numAttrs = parts > 1 ? 1 : 0;

@@ -11,8 +11,8 @@ most V / 256 + 64 additions, so log S is off by at most U A with A = 4 log V + 7
                                     U 4 A (1 + log V)
     dlogits: t = scale x - lse is rounded at the size of its terms, which p takes as a relative error; with Q = 16 +
              4 (|scale x| + |lse| + |t|): U scale Q (p (|g| + |h| (1 + |t| + H)) + [token] |g|), then the rounding to
-             the type, half a step: bf16 2^-8, fp32 2^-24 of the value, and 2^-133 (the spacing of bf16 below its
-             normal numbers; results may be flushed to zero there: 2^-126)."""
+             the type, half a step: bf16 2^-8, fp32 2^-24 of the value.  Below 2^-126 p and the result are flushed to zero:
+             2^-126 (1 + scale (|g| + |h| (1 + |t| + H)))."""
 import math
 
 import numpy as np
@@ -60,6 +60,7 @@ def forward(ctx, x, tokens, scale=1.0, k=0):
 
 def near(got, want, bound):
     got = got.double().cpu().numpy()
+    want = np.where(np.abs(want) > 3.4028235677973366e38, np.copysign(np.inf, want), want)   # past fp32's (and bf16's) range
     same = (np.isnan(got) & np.isnan(want)) | (np.isinf(want) & (got == want))
     with np.errstate(invalid="ignore"):
         bad = ~(same | (np.abs(got - want) <= bound))
@@ -107,8 +108,9 @@ def check_backward(ctx, x, tokens, scale, lse, H, g, h, in_place=False):
         tok = tokens.cpu().numpy()
         rows = np.nonzero((tok >= 0) & (tok < x.shape[1]))[0]
         one[rows, tok[rows]] = 1.0
-        bound = U * scale * Q * (p * (ga[:, None] + ha[:, None] * (1 + fin(t) + Ha[:, None])) + one * ga[:, None])
-        near(d, want, HALF[x.dtype] * fin(want) + bound + 2.0 ** -126)
+        factor = ga[:, None] + ha[:, None] * (1 + np.minimum(fin(t), 300.0) + Ha[:, None])
+        bound = U * scale * Q * (p * factor + one * ga[:, None])
+    near(d, want, HALF[x.dtype] * fin(want) + bound + 2.0 ** -126 * (1 + scale * factor))
     return d
 
 
@@ -158,12 +160,12 @@ def special_rows(vocab, dtype):
     """Rows with masks, ties, orders and numbers where a maximum, a sum or a list of the best can go wrong."""
     gen = torch.Generator().manual_seed(vocab)
     low = torch.finfo(dtype).min
-    rows = [torch.full((vocab,), -INF), torch.full((vocab,), low), torch.zeros(vocab), torch.full((vocab,), -7.5)]
+    rows = [torch.full((vocab,), v) for v in (-INF, low, 0.0, -7.5)]
     up = torch.linspace(-20, 20, vocab)
     rows += [up, up.flip(0)]                                       # every entry a new best, and the best first
     few = torch.randint(0, 3, (vocab,), generator=gen).float()     # three values only
     rows += [few, -few, torch.where(few > 0, 0.0, -0.0)]           # signs of zero
-    for value in (-INF, low):                                      # masks that leave one, three, or half
+    for value in (-INF, low, -1e30, -1e9, -1e4):                   # masks that leave one, three, or half
         for left in (1, 3, vocab // 2):
             r = torch.full((vocab,), value)
             r[torch.randperm(vocab, generator=gen)[:left]] = torch.randn(left, generator=gen)
@@ -177,6 +179,7 @@ def special_rows(vocab, dtype):
     r = torch.randn(vocab, generator=gen)
     r[vocab // 2] = 3e38
     rows.append(r)
+    rows += [torch.full((vocab,), -1e30), torch.full((vocab,), -1e9), 1e6 + 64 * torch.randn(vocab, generator=gen)]
     for bad in (float("nan"), INF):
         for at in (0, vocab // 2, vocab - 1):
             r = torch.randn(vocab, generator=gen)
@@ -244,6 +247,32 @@ def test_tokens_outside_the_vocabulary_are_reported(ctx):
     check_backward(ctx, x, tokens, 1.0, got[1], None, torch.ones(4, device=DEV), None)
     forward(ctx, x, torch.full((4,), 2 ** 31 - 1, dtype=torch.int32, device=DEV))
     assert binding.peagle_poll_status(ctx) == binding.STATUS["BAD_META"]
+
+
+@pytest.mark.parametrize("scale", [1e-20, 1e-3, 50.0, 1e20])
+def test_scales_far_from_one(ctx, scale):
+    """Nearly uniform rows, rows with one token left, and logits that the scale takes past fp32's range."""
+    x = special_rows(3001, BF16)
+    tokens = torch.arange(x.shape[0], dtype=torch.int32) * 17 % 3001
+    x, tokens = put(x), tokens.to(DEV)
+    got = forward(ctx, x, tokens, scale, 6)
+    s = x.float() * scale                                   # in fp32, as the definition has it
+    none = torch.isnan(s).any(1) | (s == INF).any(1)
+    empty = (s == -INF).all(1) & ~none
+    assert torch.isnan(got[1][none]).all() and (got[4][none] == -1).all()
+    assert (got[1][empty] == -INF).all() and (got[2][empty] == 0).all()
+    rest = ~(none | empty)
+    assert bool(rest.any())
+    keep = rest.nonzero()[:, 0]
+    check_forward(x[keep].clone(), tokens[keep], scale, 6, [None if t is None else t[keep] for t in got])
+
+
+def test_no_rows(ctx):
+    e, i = torch.empty(0, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV)
+    x = torch.empty(0, 70, dtype=BF16, device=DEV)
+    binding.peagle_token_logprobs_fwd(ctx, x, i, 1.0, e, e, e, torch.empty(0, 3, device=DEV), i.view(0, 1).expand(0, 3).contiguous())
+    binding.peagle_token_logprobs_bwd(ctx, x, i, 1.0, e, e, e, e, x.clone())
+    torch.cuda.synchronize()
 
 
 def test_outputs_are_optional_and_repeat(ctx):

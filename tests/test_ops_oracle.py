@@ -186,7 +186,8 @@ def _norm_call(lib, ctx, back, **over):
 
 @pytest.mark.parametrize("back", [False, True])
 @pytest.mark.parametrize("over,status", [
-    ({"rows": 0}, "OK"), ({"rows": -1}, "BAD_SHAPE"), ({"cols": 0}, "BAD_SHAPE"), ({"kind": 2}, "BAD_SHAPE"),
+    ({"rows": 0}, "OK"), ({"rows": -1}, "BAD_SHAPE"), ({"cols": 0}, "BAD_SHAPE"),
+    ({"cols": (1 << 30) + 1, "ldx": 1 << 31, "ldy": 1 << 31, "lddy": 1 << 31}, "TOO_LARGE"), ({"kind": 2}, "BAD_SHAPE"),
     ({"kind": -1}, "BAD_SHAPE"), ({"x_dtype": 2}, "BAD_SHAPE"), ({"w_dtype": -1}, "BAD_SHAPE"), ({"ldx": 63}, "BAD_SHAPE"),
     ({"ldy": 63}, "BAD_SHAPE"), ({"X": 0}, "NULL"), ({"Y": 0}, "NULL"), ({"X": 4097}, "ALIGN"), ({"Y": 8193}, "ALIGN"),
     ({"x_dtype": 0, "X": 4098}, "ALIGN"), ({"weight": 4097}, "ALIGN"), ({"rstd": 12290}, "ALIGN"),
@@ -227,7 +228,7 @@ def _logprob_call(lib, ctx, back, **over):
 @pytest.mark.parametrize("over,status", [
     ({"rows": 0}, "OK"), ({"rows": -2}, "BAD_SHAPE"), ({"vocab": 0}, "BAD_SHAPE"), ({"ld": 99}, "BAD_SHAPE"),
     ({"dtype": 5}, "BAD_SHAPE"), ({"vocab": (1 << 30) + 1, "ld": 1 << 31, "ldd": 1 << 31}, "TOO_LARGE"), ({"scale": 0.0}, "BAD_SHAPE"), ({"scale": -1.0}, "BAD_SHAPE"),
-    ({"scale": float("nan")}, "BAD_SHAPE"), ({"scale": float("inf")}, "BAD_SHAPE"), ({"logits": 0}, "NULL"),
+    ({"scale": float("nan")}, "BAD_SHAPE"), ({"scale": float("inf")}, "BAD_SHAPE"), ({"scale": 1e-21}, "BAD_SHAPE"), ({"logits": 0}, "NULL"),
     ({"tokens": 0}, "NULL"), ({"logits": 4097}, "ALIGN"), ({"tokens": 8194}, "ALIGN"), ({"lse": 16386}, "ALIGN"),
 ])
 def test_logprob_refusals(lib, zeros, back, over, status):
