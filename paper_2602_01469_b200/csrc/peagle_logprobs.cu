@@ -629,7 +629,9 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
 
 // ------------------------------------------------------------------ backward
 
-constexpr int BWD_PIECES = 4; // 16-byte pieces per thread
+// 16-byte pieces per thread.  They are read and written as data that is not used again: 4,096 rows of 128,000 bf16 take
+// 330 us, through ordinary accesses 366.
+constexpr int BWD_PIECES = 4;
 
 // A block per BWD_PIECES * LP_THREADS pieces of a row.
 template <class T>
@@ -679,7 +681,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
 #pragma unroll
         for (int u = 0; u < BWD_PIECES; ++u)
             if (first + u * LP_THREADS < pieces)
-                p[u].v = *reinterpret_cast<const uint4 *>(row - before + (size_t)(first + u * LP_THREADS) * N);
+                p[u].v = __ldcs(reinterpret_cast<const uint4 *>(row - before + (size_t)(first + u * LP_THREADS) * N));
     }
 #pragma unroll
     for (int u = 0; u < BWD_PIECES; ++u) {
@@ -703,7 +705,7 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
             else
                 w = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
                                pack_bf16x2(v[6], v[7]));
-            *reinterpret_cast<uint4 *>(out + id) = w;
+            __stcs(reinterpret_cast<uint4 *>(out + id), w);
         } else {
 #pragma unroll
             for (int e = 0; e < N; ++e)
