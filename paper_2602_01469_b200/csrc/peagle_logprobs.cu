@@ -634,7 +634,7 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
 constexpr int BWD_PIECES = 4;
 
 // A block per BWD_PIECES * LP_THREADS pieces of a row.
-template <class T>
+template <class T, bool ENTROPY>
 __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_constant__ LogprobArgs a, int parts)
 {
     constexpr int N = Piece<T>::N;
@@ -643,19 +643,13 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
     T *out = static_cast<T *>(a.dlogits) + (size_t)r * a.ldd;
     const int token = a.g_lp ? a.tokens[r] : -1;
     const bool given = token >= 0 && token < a.vocab;
-    const float g = given ? a.g_lp[r] : 0.f, h = a.g_h ? a.g_h[r] : 0.f, lse = a.lse_in[r];
-    const float H = a.g_h ? a.entropy_in[r] : 0.f;
+    const float g = given ? a.g_lp[r] : 0.f, h = ENTROPY ? a.g_h[r] : 0.f, lse = a.lse_in[r];
+    const float H = ENTROPY ? a.entropy_in[r] : 0.f;
     const bool zero = (g == 0.f && h == 0.f) || lse == -INF;
-    // of t = log p = scale x - lse
-    const auto gradient = [&](float t, bool token_here) {
+    // the token's own entry, of t = log p: 1 - p without the digits that p near 1 would take
+    const auto of_token = [&](float t) {
         const float p = fast_exp2(t * LOG2E);
-        float v = -g;
-        if (a.g_h)
-            v = fmaf(-h, fmaxf(t, T_FLOOR) + H, v);
-        v *= p;
-        if (token_here) // 1 - p without the digits that p near 1 would take
-            v = -g * expm1f(t) - p * h * (fmaxf(t, T_FLOOR) + H);
-        return v * a.scale;
+        return a.scale * (-g * expm1f(t) - (ENTROPY ? p * h * (fmaxf(t, T_FLOOR) + H) : 0.f));
     };
     if (!zero && fabsf(lse) >= LSE_LARGE) {
         // from the row itself: one block, so that dlogits may be logits
@@ -668,8 +662,10 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
             S += fast_exp2((to_f32(row[j]) - m) * a.scale * LOG2E);
         const float logS = logf(block_join(S, [](float p, float q) { return p + q; }));
-        for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
-            from_f32(out + j, gradient((to_f32(row[j]) - m) * a.scale - logS, j == token));
+        for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
+            const float t = (to_f32(row[j]) - m) * a.scale - logS, p = fast_exp2(t * LOG2E);
+            from_f32(out + j, j == token ? of_token(t) : a.scale * p * (-g - h * (fmaxf(t, T_FLOOR) + H)));
+        }
         return;
     }
     const int before = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(T));
@@ -683,20 +679,39 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
             if (first + u * LP_THREADS < pieces)
                 p[u].v = __ldcs(reinterpret_cast<const uint4 *>(row - before + (size_t)(first + u * LP_THREADS) * N));
     }
+    // v = p (c0 + c1 t)
+    const float c1 = -h * a.scale, c0 = fmaf(c1, H, -g * a.scale);
+    const F2 scale2 = f2(a.scale, a.scale), minus = f2(-lse, -lse), log2e = f2(LOG2E, LOG2E);
 #pragma unroll
     for (int u = 0; u < BWD_PIECES; ++u) {
         const int i = first + u * LP_THREADS, id = i * N - before;
         if (i >= pieces)
             break;
         float v[N];
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            v[e] = zero ? 0.f : gradient(fmaf(p[u].get(e), a.scale, -lse), false);
-        if ((unsigned)(token - id) < (unsigned)N && !zero) {
+        if (zero) {
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (id + e == token)
-                    v[e] = gradient(fmaf(p[u].get(e), a.scale, -lse), true);
+                v[e] = 0.f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; e += 2) {
+                const F2 t = fma_f2(f2(p[u].get(e), p[u].get(e + 1)), scale2, minus);
+                const float2 t2 = unf2(mul_f2(t, log2e)), tv = unf2(t);
+                const F2 prob = f2(fast_exp2(t2.x), fast_exp2(t2.y));
+                F2 w = f2(c0, c0);
+                if (ENTROPY)
+                    w = fma_f2(f2(c1, c1), f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR)), w);
+                const float2 d = unf2(mul_f2(prob, w));
+                v[e] = d.x;
+                v[e + 1] = d.y;
+            }
+            if ((unsigned)(token - id) < (unsigned)N && given) {
+                const float own = of_token(fmaf(to_f32(row[token]), a.scale, -lse));
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (id + e == token)
+                        v[e] = own;
+            }
         }
         if (alike && id >= 0 && id + N <= a.vocab) {
             uint4 w;
@@ -790,7 +805,10 @@ int backward_of(const LogprobArgs &a, cudaStream_t s)
     const int parts = (int)((pieces + BWD_PIECES * LP_THREADS - 1) / (BWD_PIECES * LP_THREADS));
     if ((int64_t)a.rows * parts > INT32_MAX)
         return PEAGLE_ERR_TOO_LARGE;
-    logprobs_bwd_kernel<T><<<(unsigned)a.rows * parts, LP_THREADS, 0, s>>>(a, parts);
+    if (a.g_h)
+        logprobs_bwd_kernel<T, true><<<(unsigned)a.rows * parts, LP_THREADS, 0, s>>>(a, parts);
+    else
+        logprobs_bwd_kernel<T, false><<<(unsigned)a.rows * parts, LP_THREADS, 0, s>>>(a, parts);
     return 1;
 }
 
