@@ -14,9 +14,10 @@
 // Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
 // k-th largest of the maxima of 64 groups of threads, then the k-th best entry so far).  A chunk's maximum, which the
 // sums need anyway, says whether a thread has anything to add; what reaches the bound goes to a list in shared memory,
-// which is cut to its k best when it has grown by half.  A chunk that does not fit the list (rows in ascending order, or of
-// equal entries) is gone through again with the bound that the list gives.  Entries are compared by value, then by id,
-// so the result does not depend on the order in which they came.
+// which is cut to its k best when it has grown by half.  The block's warps meet for that only once in four chunks.  A row
+// that brings more than the list holds in that time (in ascending order, or of equal entries) is begun again, with a
+// meeting for every chunk; a chunk that does not fit even so is gone through again with the bound that the list gives.
+// Entries are compared by value, then by id, so the result does not depend on the order in which they came.
 #include <cuda_bf16.h>
 
 #include <algorithm>
@@ -37,6 +38,7 @@ constexpr int FWD_PIECES = 4; // 16-byte pieces per thread and chunk
 constexpr int GROUPS = 64;     // of threads, whose maxima give the first bound
 constexpr int STAGES = 2;     // chunks on their way or at hand
 constexpr int LIST = 1024;    // entries of the list of candidates
+constexpr int MEET_EVERY = 4; // chunks between two looks at the list
 constexpr int COUNTED = 512; // entries that are ranked by counting, at most
 constexpr int LEAST_PART = 4096; // entries of a row's part
 static_assert(GROUPS >= PEAGLE_MAX_TOP_K && LP_THREADS % GROUPS == 0, "a first bound for every k");
@@ -337,10 +339,10 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
     // whole 16-byte pieces that hold an entry of this part; `before` entries of the first belong elsewhere
     const int before = (int)(reinterpret_cast<uintptr_t>(row + begin) % 16 / sizeof(T));
     const int pieces = n ? (before + n + N - 1) / N : 0;
-    const T *x = row + begin - before + threadIdx.x * N; // this thread's first piece of the next chunk to be fetched
     const float l = a.scale * LOG2E;
     const uint32_t ring_at = smem_u32(ring + threadIdx.x);
 
+    const T *x = row; // this thread's first piece of the next chunk to be fetched
     const auto fetch = [&](int first, int stage) {
 #pragma unroll
         for (int u = 0; u < U; ++u)
@@ -351,177 +353,202 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
         asm volatile("cp.async.commit_group;" ::: "memory");
         x += STEP * N;
     };
-#pragma unroll
-    for (int i = 0; i < STAGES; ++i)
-        fetch(i * STEP, i);
-    if (TOP && threadIdx.x == 0)
-        count = 0;
-    Sums s = {-INF, 0.f, 0.f};
-    float bound = -INF; // an entry at or above it may be among the k best
+    Sums s;
     // A list that has grown by half is cut.  (4,096 rows of 128,000, k = 20: 264 us; when it has tripled 275.)  A short
     // part ends before that pays.
     const int long_list = pieces <= 4 * STEP ? max(LP_THREADS - 8, a.top_k + a.top_k / 2) : a.top_k + a.top_k / 2 + 6;
-    int stage = 0;
-    for (int first = 0; first < pieces; first += STEP) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
-        const uint4 *at = ring + stage * STEP + threadIdx.x;
-        Piece<T> now[U];
+    // Looking at the list means that all warps wait for the slowest.  (4,096 rows of 128,000 bf16, k = 8: 256 us with a
+    // look at every chunk, 243 at every fourth; 2,048 rows of fp32 213 and 203.)  A row that overflows the list unseen
+    // is begun again.
+    for (int every = MEET_EVERY;; every = 1) {
+        x = row + begin - before + threadIdx.x * N;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            now[u].v = at[u * LP_THREADS];
-        if (first == 0 || first + STEP >= pieces) { // with the first piece, the last, or none
+        for (int i = 0; i < STAGES; ++i)
+            fetch(i * STEP, i);
+        if (TOP && threadIdx.x == 0)
+            count = 0;
+        s = {-INF, 0.f, 0.f};
+        float bound = -INF; // an entry at or above it may be among the k best
+        int end = 0;        // how far this thread has filled the list since the warps met
+        bool overflow = false;
+        int stage = 0;
+        for (int first = 0; first < pieces; first += STEP) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(STAGES - 1) : "memory");
+            const uint4 *at = ring + stage * STEP + threadIdx.x;
+            Piece<T> now[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int i = first + u * LP_THREADS + threadIdx.x;
-                if (i == 0 || i >= pieces - 1)
-                    now[u].mask(i < pieces ? before - i * N : N, before + n - i * N);
-            }
-        }
-        uint32_t most[U], all = piece_max(now[0]);
-        most[0] = all;
+            for (int u = 0; u < U; ++u)
+                now[u].v = at[u * LP_THREADS];
+            if (first == 0 || first + STEP >= pieces) { // with the first piece, the last, or none
 #pragma unroll
-        for (int u = 1; u < U; ++u) {
-            most[u] = piece_max(now[u]);
-            all = max_words<T>(all, most[u]);
-        }
-        const float top = of_max_word<T>(all);
-        if (top > s.m)
-            rescale(s, top, l);
-        const float c = reference(s.m, l);
-        // Entries whose probability is zero in any case are raised to where 0 times their t is 0: as pairs of bf16
-        // here, else one by one.  The second term is more than the rounding to bf16 takes off.  (Beside a maximum
-        // near the end of the type's range there is no room for that: see below.)
-        const float from = s.m == -INF ? 0.f : s.m;
-        const float low = fabsf(from) < 1e37f ? fmaf(fabsf(from), -0x1p-6f, from + T_FLOOR / l) : -INF;
-        const uint32_t low2 = pack_bf16x2(low, low);
-        const F2 l2 = f2(l, l), minus = f2(-c, -c);
-        F2 S2 = f2(s.S, 0.f), E2 = f2(s.E, 0.f);
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int e = 0; e < N; e += 2) {
-                F2 v;
-                if constexpr (ENTROPY && N == 8) {
-                    const uint32_t w = raised(now[u].word(e / 2), low2);
-                    v = f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-                } else {
-                    v = f2(now[u].get(e), now[u].get(e + 1));
+                for (int u = 0; u < U; ++u) {
+                    const int i = first + u * LP_THREADS + threadIdx.x;
+                    if (i == 0 || i >= pieces - 1)
+                        now[u].mask(i < pieces ? before - i * N : N, before + n - i * N);
                 }
-                F2 t = fma_f2(v, l2, minus);
-                const float2 tv = unf2(t);
-                const F2 p = f2(fast_exp2(tv.x), fast_exp2(tv.y));
-                S2 = add_f2(S2, p);
-                if (ENTROPY && N == 4)
-                    t = f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR));
-                if (ENTROPY)
-                    E2 = fma_f2(p, t, E2);
             }
-        const float2 Sv = unf2(S2), Ev = unf2(E2);
-        s.S = Sv.x + Sv.y;
-        if constexpr (ENTROPY && N == 8) {
-            const float E = Ev.x + Ev.y;
-            if (E != E && s.S == s.S) {
+            uint32_t most[U], all = piece_max(now[0]);
+            most[0] = all;
+#pragma unroll
+            for (int u = 1; u < U; ++u) {
+                most[u] = piece_max(now[u]);
+                all = max_words<T>(all, most[u]);
+            }
+            const float top = of_max_word<T>(all);
+            if (top > s.m)
+                rescale(s, top, l);
+            const float c = reference(s.m, l);
+            // Entries whose probability is zero in any case are raised to where 0 times their t is 0: as pairs of bf16
+            // here, else one by one.  The second term is more than the rounding to bf16 takes off.  (Beside a maximum
+            // near the end of the type's range there is no room for that: see below.)
+            const float from = s.m == -INF ? 0.f : s.m;
+            const float low = fabsf(from) < 1e37f ? fmaf(fabsf(from), -0x1p-6f, from + T_FLOOR / l) : -INF;
+            const uint32_t low2 = pack_bf16x2(low, low);
+            const F2 l2 = f2(l, l), minus = f2(-c, -c);
+            F2 S2 = f2(s.S, 0.f), E2 = f2(s.E, 0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int e = 0; e < N; e += 2) {
+                    F2 v;
+                    if constexpr (ENTROPY && N == 8) {
+                        const uint32_t w = raised(now[u].word(e / 2), low2);
+                        v = f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+                    } else {
+                        v = f2(now[u].get(e), now[u].get(e + 1));
+                    }
+                    F2 t = fma_f2(v, l2, minus);
+                    const float2 tv = unf2(t);
+                    const F2 p = f2(fast_exp2(tv.x), fast_exp2(tv.y));
+                    S2 = add_f2(S2, p);
+                    if (ENTROPY && N == 4)
+                        t = f2(fmaxf(tv.x, T_FLOOR), fmaxf(tv.y, T_FLOOR));
+                    if (ENTROPY)
+                        E2 = fma_f2(p, t, E2);
+                }
+            const float2 Sv = unf2(S2), Ev = unf2(E2);
+            s.S = Sv.x + Sv.y;
+            if constexpr (ENTROPY && N == 8) {
+                const float E = Ev.x + Ev.y;
+                if (E != E && s.S == s.S) {
 #pragma unroll 1
-                for (int i = 0; i < U * N; ++i) {
-                    const int id = (first + i / N * LP_THREADS + (int)threadIdx.x) * N + i % N - before;
-                    const float t = fmaf(to_f32(reinterpret_cast<const T *>(at + i / N * LP_THREADS)[i % N]), l, -c);
-                    if (id >= 0 && id < n)
-                        s.E = fmaf(fast_exp2(t), fmaxf(t, T_FLOOR), s.E);
+                    for (int i = 0; i < U * N; ++i) {
+                        const int id = (first + i / N * LP_THREADS + (int)threadIdx.x) * N + i % N - before;
+                        const float t = fmaf(to_f32(reinterpret_cast<const T *>(at + i / N * LP_THREADS)[i % N]), l, -c);
+                        if (id >= 0 && id < n)
+                            s.E = fmaf(fast_exp2(t), fmaxf(t, T_FLOOR), s.E);
+                    }
+                } else {
+                    s.E = E;
                 }
             } else {
-                s.E = E;
+                s.E = Ev.x + Ev.y;
             }
-        } else {
-            s.E = Ev.x + Ev.y;
-        }
-        if constexpr (TOP) {
-            const int k = a.top_k;
-            if (first == 0) { // the k-th largest of the maxima of 64 groups of threads
-                constexpr int LANES = LP_THREADS / GROUPS;
-                float most = top;
+            if constexpr (TOP) {
+                const int k = a.top_k;
+                if (first == 0) { // the k-th largest of the maxima of 64 groups of threads
+                    constexpr int LANES = LP_THREADS / GROUPS;
+                    float most = top;
 #pragma unroll
-                for (int o = 1; o < LANES; o *= 2)
-                    most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-                if (threadIdx.x % LANES == 0)
-                    reinterpret_cast<float *>(first_max)[threadIdx.x / LANES] = most;
-                __syncthreads();
-                if (threadIdx.x < GROUPS) {
-                    most = reinterpret_cast<float *>(first_max)[threadIdx.x];
-                    int above = 0, equal = 0;
-#pragma unroll
-                    for (int i = 0; i < GROUPS / 4; ++i) {
-                        const float4 o = first_max[i];
-                        above += (o.x > most) + (o.y > most) + (o.z > most) + (o.w > most);
-                        equal += (o.x == most) + (o.y == most) + (o.z == most) + (o.w == most);
-                    }
-                    if (above < k && above + equal >= k)
-                        first_bound = most;
-                }
-                __syncthreads();
-                bound = first_bound;
-            }
-            uint64_t least = 0;
-            while (true) {
-                int end = 0;
-                if (top >= bound) {
-                    // which of the entries reach the bound, without a branch among a piece's: a thread on this path
-                    // keeps its whole block waiting
-                    uint32_t reach = 0;
-#pragma unroll
-                    for (int u = 0; u < U; ++u)
-                        if (of_max_word<T>(most[u]) >= bound) {
-                            Piece<T> p;
-                            p.v = at[u * LP_THREADS];
-#pragma unroll
-                            for (int e = 0; e < N; ++e)
-                                reach |= (uint32_t)(p.get(e) >= bound) << (u * N + e);
-                        }
-                    for (; reach; reach &= reach - 1) {
-                        const int i = __ffs(reach) - 1, u = i / N, e = i % N;
-                        const int id = (first + u * LP_THREADS + (int)threadIdx.x) * N + e - before;
-                        const float v = to_f32(reinterpret_cast<const T *>(at + u * LP_THREADS)[e]);
-                        const uint64_t key = rank_key(v, begin + id);
-                        if (id >= 0 && id < n && key >= least) {
-                            const int place = atomicAdd(&count, 1);
-                            if (place < LIST)
-                                list[place] = key;
-                            end = place + 1;
-                        }
-                    }
-                }
-                if (!__syncthreads_or(end > long_list)) {
-                    if (first == 0)
-                        bound = from_key(order_key(bound) + 1); // k entries of this chunk, with lower ids, reach it
-                    break;
-                }
-                if (count <= LIST) {
-                    cut_list(list, count, k);
-                    if (threadIdx.x == 0)
-                        count = k;
-                    bound = from_key((uint32_t)(list[k - 1] >> 32) + 1); // the k best have lower ids than what follows
+                    for (int o = 1; o < LANES; o *= 2)
+                        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                    if (threadIdx.x % LANES == 0)
+                        reinterpret_cast<float *>(first_max)[threadIdx.x / LANES] = most;
                     __syncthreads();
-                    break;
+                    if (threadIdx.x < GROUPS) {
+                        most = reinterpret_cast<float *>(first_max)[threadIdx.x];
+                        int above = 0, equal = 0;
+#pragma unroll
+                        for (int i = 0; i < GROUPS / 4; ++i) {
+                            const float4 o = first_max[i];
+                            above += (o.x > most) + (o.y > most) + (o.z > most) + (o.w > most);
+                            equal += (o.x == most) + (o.y == most) + (o.z == most) + (o.w == most);
+                        }
+                        if (above < k && above + equal >= k)
+                            first_bound = most;
+                    }
+                    __syncthreads();
+                    bound = first_bound;
                 }
-                // once more, for what reaches the k-th best of those that found a place
-                least = kth_best(list, LIST, k);
-                uint64_t mine[LIST / LP_THREADS];
+                uint64_t least = 0;
+                while (true) {
+                    if (top >= bound) {
+                        // which of the entries reach the bound, without a branch among a piece's: a thread on this path
+                        // keeps its whole block waiting
+                        uint32_t reach = 0;
 #pragma unroll
-                for (int j = 0; j < LIST / LP_THREADS; ++j)
-                    mine[j] = list[threadIdx.x + j * LP_THREADS];
-                __syncthreads();
-                if (threadIdx.x == 0)
-                    count = 0;
-                __syncthreads();
-                const int chunk_id = begin + first * N - before;
+                        for (int u = 0; u < U; ++u)
+                            if (of_max_word<T>(most[u]) >= bound) {
+                                Piece<T> p;
+                                p.v = at[u * LP_THREADS];
 #pragma unroll
-                for (int j = 0; j < LIST / LP_THREADS; ++j)
-                    if (mine[j] >= least && (int)~(uint32_t)mine[j] < chunk_id) // from the chunks before
-                        list[atomicAdd(&count, 1)] = mine[j];
-                bound = from_key((uint32_t)(least >> 32));
+                                for (int e = 0; e < N; ++e)
+                                    reach |= (uint32_t)(p.get(e) >= bound) << (u * N + e);
+                            }
+                        for (; reach; reach &= reach - 1) {
+                            const int i = __ffs(reach) - 1, u = i / N, e = i % N;
+                            const int id = (first + u * LP_THREADS + (int)threadIdx.x) * N + e - before;
+                            const float v = to_f32(reinterpret_cast<const T *>(at + u * LP_THREADS)[e]);
+                            const uint64_t key = rank_key(v, begin + id);
+                            if (id >= 0 && id < n && key >= least) {
+                                const int place = atomicAdd(&count, 1);
+                                if (place < LIST)
+                                    list[place] = key;
+                                end = place + 1;
+                            }
+                        }
+                    }
+                    const bool meet = first / STEP % every == every - 1;
+                    if (!meet || !__syncthreads_or(end > long_list)) {
+                        if (meet)
+                            end = 0;
+                        if (first == 0)
+                            bound = from_key(order_key(bound) + 1); // k entries of this chunk, with lower ids, reach it
+                        break;
+                    }
+                    end = 0;
+                    if (count <= LIST) {
+                        cut_list(list, count, k);
+                        if (threadIdx.x == 0)
+                            count = k;
+                        bound = from_key((uint32_t)(list[k - 1] >> 32) + 1); // the k best have lower ids than what follows
+                        __syncthreads();
+                        break;
+                    }
+                    if (every > 1) {
+                        overflow = true;
+                        break;
+                    }
+                    // once more, for what reaches the k-th best of those that found a place
+                    least = kth_best(list, LIST, k);
+                    uint64_t mine[LIST / LP_THREADS];
+#pragma unroll
+                    for (int j = 0; j < LIST / LP_THREADS; ++j)
+                        mine[j] = list[threadIdx.x + j * LP_THREADS];
+                    __syncthreads();
+                    if (threadIdx.x == 0)
+                        count = 0;
+                    __syncthreads();
+                    const int chunk_id = begin + first * N - before;
+#pragma unroll
+                    for (int j = 0; j < LIST / LP_THREADS; ++j)
+                        if (mine[j] >= least && (int)~(uint32_t)mine[j] < chunk_id) // from the chunks before
+                            list[atomicAdd(&count, 1)] = mine[j];
+                    bound = from_key((uint32_t)(least >> 32));
+                }
             }
+            if (TOP && overflow)
+                break;
+            fetch(first + STAGES * STEP, stage);
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
-        fetch(first + STAGES * STEP, stage);
-        stage = stage + 1 == STAGES ? 0 : stage + 1;
+        if (!TOP)
+            break;
+        __syncthreads();
+        if (count <= LIST)
+            break;
+        asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads(); // everybody has seen the count
     }
 
     // join the threads' sums, then the blocks'

@@ -208,6 +208,23 @@ def test_rows_where_it_can_go_wrong(ctx, dtype, vocab, k, repeat):
     check_backward(ctx, x, tokens, 1.0, got[1], None, g, None)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("repeat", [1, 130]) # rows cut into parts, and whole ones
+def test_rows_that_overflow_the_list_late(ctx, dtype, repeat):
+    vocab, k = 20011, 20
+    gen = torch.Generator().manual_seed(5)
+    rows = []
+    for at in (2048, 9000, 15000, 17500, vocab - 1100):
+        for tail in (torch.linspace(10, 30, vocab - at), torch.full((vocab - at,), 12.0)):
+            r = torch.randn(vocab, generator=gen)
+            r[at:] = tail
+            rows.append(r)
+    x = torch.stack(rows).repeat(repeat, 1).to(dtype)
+    tokens = torch.randint(-1, vocab, (x.shape[0],), generator=gen).to(torch.int32).to(DEV)
+    x = put(x, 0, 0)
+    check_forward(x, tokens, 0.9, k, forward(ctx, x, tokens, 0.9, k))
+
+
 def test_a_peaked_row_keeps_its_digits(ctx):
     """Large logits and a probability near one: neither logprob nor 1 - p is a difference of rounded numbers."""
     x = torch.full((2, 5000), 20.0)
