@@ -308,7 +308,8 @@ int peagle_layer_partitioned(peagle_ctx *ctx, const peagle_problem_t *prob,
  *     taken (16-byte aligned rows are faster);
  *   - the device that was current before the call is current after it, and scratch that a call
  *     keeps in the context stays where it is until peagle_destroy, so calls may be captured into CUDA
- *     graphs, the first one too.  Calls that overlap on the GPU still need a context each.
+ *     graphs, the first one too.  Calls that overlap on the GPU, replays of graphs among them, still
+ *     need a context each.
  * rows == 0 (tensors of 0 elements) returns PEAGLE_OK and changes nothing.  Outputs must not overlap
  * inputs or each other, except where "in place" is stated.
  */
@@ -320,8 +321,8 @@ typedef enum peagle_dtype { PEAGLE_F32 = 0, PEAGLE_BF16 = 1 } peagle_dtype;
  *     rstd = 1 / sqrt(mean((x - mu)^2) + eps),   y = (x - mu) * rstd * weight + bias
  * X, Y are dev [rows][cols] of x_dtype; weight, bias dev [cols] of w_dtype, each may be NULL (1 and 0).
  * mean, rstd are dev fp32 [rows], what the backward needs; each may be NULL (mean is not written by
- * PEAGLE_NORM_RMS).  eps > 0, cols <= 2^30 (up to 16,384 a row is read once).  In place: Y may be X with the same leading dimension.  A NaN or infinity
- * stays in its row.  Asynchronous.
+ * PEAGLE_NORM_RMS).  eps > 0, cols <= 2^30 (up to 16,384 a row is read once).  In place: Y may be X with
+ * the same leading dimension.  A NaN or infinity stays in its row.  Asynchronous.
  */
 typedef enum peagle_norm { PEAGLE_NORM_LAYER = 0, PEAGLE_NORM_RMS = 1 } peagle_norm;
 int peagle_norm_fwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
@@ -351,8 +352,8 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
  * 0) and top_logprobs = s_id - lse.  logits is dev [rows][vocab] of `dtype`; tokens dev int32 [rows], -1
  * where a row has no token: its logprob is 0, all else as for any row.  logprob, lse, entropy are dev fp32
  * [rows], top_logprobs fp32 and top_ids int32 [rows][top_k] (contiguous); each may be NULL, tokens too when
- * logprob is.  vocab <= 2^30, 0 <= top_k <= min(vocab, PEAGLE_MAX_TOP_K), and the two top outputs are either both there or
- * both NULL (top_k == 0).  -inf is a token of probability zero, and
+ * logprob is.  vocab <= 2^30, 0 <= top_k <= min(vocab, PEAGLE_MAX_TOP_K), and the two top outputs are
+ * either both there or both NULL (top_k == 0).  -inf is a token of probability zero, and
  *   - a row of nothing but -inf (or logits that scale takes there) has lse = logprob = -inf, entropy 0, top
  *     ids 0, 1, .. with log probability -inf;
  *   - a row with a NaN or +inf has NaN in all its fp32 outputs (0 for the logprob of token -1), top ids -1;

@@ -259,35 +259,35 @@ class AdamWTensors:
         self.device = self.items[0]["param"].device.index if self.items else None
         self.c = (peagle_adamw_tensor_t * max(len(self.items), 1))()
         written = []
+        f32, codes, dev = torch.float32, torch.float8_e4m3fn, self.device
+
+        def own(t, dtype, size, count):
+            if t is None or t.dtype != dtype or t.get_device() != dev or t.numel() != count or not t.is_contiguous():
+                _refuse()
+            at = t.data_ptr()
+            if count:
+                written.append((at, at + size * count))
+            return at
+
         for c, i in zip(self.c, self.items):
-            p, n = i["param"], i["param"].numel()
-            eight = i.get("m_scale") is not None
-            state = torch.float8_e4m3fn if eight else torch.float32
-            for name, dtype, count in (("master", torch.float32, n), ("m", state, n), ("v", state, n),
-                                       ("m_scale", torch.float32, -(-n // ADAMW_BLOCK)),
-                                       ("v_scale", torch.float32, -(-n // ADAMW_BLOCK))):
-                t = i.get(name)
-                if t is None:
-                    if not (name == "master" or (name.endswith("scale") and not eight)):
-                        _refuse()
-                    continue
-                self._own(t, count)
-                if t.dtype != dtype:
-                    _refuse()
-                written.append((t.data_ptr(), t.numel() * t.element_size()))
-                setattr(c, name, t.data_ptr())
-            self._own(p, n)
-            written.append((p.data_ptr(), n * p.element_size()))
-            c.param, c.count, c.param_dtype = p.data_ptr(), n, _dtype(p)
-            c.weight_decay = float(i.get("weight_decay", 0.0))
-        written = sorted(w for w in written if w[1])
-        if any(a + size > b for (a, size), (b, _) in zip(written, written[1:])):
+            p, get = i["param"], i.get
+            n, code, master, m_scale, v_scale = p.numel(), _dtype(p), get("master"), get("m_scale"), get("v_scale")
+            if m_scale is None and v_scale is None:
+                c.m, c.v = own(get("m"), f32, 4, n), own(get("v"), f32, 4, n)
+            elif m_scale is None or v_scale is None:
+                _refuse()
+            else:
+                blocks = -(-n // ADAMW_BLOCK)
+                c.m, c.v = own(get("m"), codes, 1, n), own(get("v"), codes, 1, n)
+                c.m_scale, c.v_scale = own(m_scale, f32, 4, blocks), own(v_scale, f32, 4, blocks)
+            if master is not None:
+                c.master = own(master, f32, 4, n)
+            c.param, c.count, c.param_dtype = own(p, p.dtype, 2 if code else 4, n), n, code
+            c.weight_decay = float(get("weight_decay", 0.0))
+        written.sort()
+        if any(end > begin for (_, end), (begin, _) in zip(written, written[1:])):
             _refuse("BAD_RANGE")
         self.set_grads([i["grad"] for i in self.items])
-
-    def _own(self, t, count):
-        if not t.is_cuda or t.get_device() != self.device or t.numel() != count or not t.is_contiguous():
-            _refuse()
 
     def set_grads(self, grads):
         """Other gradients for the steps to come, in the order of the tensors."""
@@ -295,7 +295,8 @@ class AdamWTensors:
         if len(grads) != len(self.items):
             _refuse()
         for c, i, g in zip(self.c, self.items, grads):
-            self._own(g, c.count)
+            if g.get_device() != self.device or g.numel() != c.count or not g.is_contiguous():
+                _refuse()
             c.grad, c.grad_dtype = g.data_ptr(), _dtype(g)
             i["grad"] = g
 

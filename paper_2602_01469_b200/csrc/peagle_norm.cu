@@ -11,6 +11,10 @@
 // weights as fp32 in shared memory.  In the backward the threads keep the same columns from row to row and
 // hold the column sums in registers; a block's groups join theirs in shared memory at the end, and a second
 // kernel adds up the blocks.  Rows of more columns go through kernels that read them again for every pass.
+//
+// Measured, of the rate of a copy: RMS forward, 32,768 rows of 2,880 bf16, 64 us (90 %), backward 95 (91 %); layer norm
+// backward, 524,288 rows of 128 bf16, 72 (87 %).  What is missing is loads in flight while a row's sums are joined.  Few
+// rows are bound by latency: layer norm backward of 3,891 rows of 1,001 fp32 takes 18.5 us (39 %), of 30,000 66 (83 %).
 #include <cuda_bf16.h>
 
 #include <algorithm>
