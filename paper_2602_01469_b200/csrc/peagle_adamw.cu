@@ -14,7 +14,7 @@
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, about 70 per element and half of them integer ones for the random bits and the
-// roundings: 91 M elements, bf16, take 238 us, 59 % of the copy rate.  A first version had 113 and took 343; it formed
+// roundings: 91 M elements, bf16, take 229 us, 61 % of the copy rate.  A first version had 113 and took 343; it formed
 // the new m and v in fp64 so that the codes would not depend on how the arithmetic is ordered.  In fp32 two or three
 // codes in a million fall on the other side of the random bits, which is as good a rounding; only a block's scale has
 // to be right, and where a block's largest number lies at a power of two, or is not finite, the largest is found
@@ -83,12 +83,16 @@ constexpr int SHORT_LIST = 32; // tensors of a smaller kernel parameter, which t
 static_assert(sizeof(Table<PEAGLE_ADAMW_TENSORS>) <= 32764, "kernel parameters");
 
 // Scrambles 32 bits: two rounds of shift-xor and multiplication by an odd number, each of them one to one.
-__host__ __device__ inline uint32_t mix(uint32_t x)
+__host__ __device__ inline uint32_t mix_but_for_the_last(uint32_t x)
 {
     x ^= x >> 16;
     x *= 0x7FEB352Du;
     x ^= x >> 15;
-    x *= 0x846CA68Bu;
+    return x * 0x846CA68Bu;
+}
+__host__ __device__ inline uint32_t mix(uint32_t x)
+{
+    x = mix_but_for_the_last(x);
     return x ^ x >> 16;
 }
 
@@ -216,9 +220,10 @@ __device__ __forceinline__ float small_code(float y, float large, uint32_t bits2
     const float z = __uint_as_float((__float_as_uint(a + 0.015625f) + bits20) & 0xfff00000u) - 0.015625f;
     return a != a ? a : copysignf(keep && a > 0.f ? fmaxf(z, 0.001953125f) : z, y); // 2^-9
 }
-// The 20 bits of an element's random 32 for m and for the root: 16 of them and a half.
-__device__ __forceinline__ uint32_t bits_of_m(uint32_t bits) { return (bits << 4 & 0xffff0u) | 8u; }
-__device__ __forceinline__ uint32_t bits_of_root(uint32_t bits) { return (bits >> 12 & 0xffff0u) | 8u; }
+// The 20 bits of an element for m and for the root: the lower and the upper 16 of mix(), and a half.  From what mix()
+// has before its last step, which leaves the upper ones as they are: 91 M elements 229 us, from mix() itself 238.
+__device__ __forceinline__ uint32_t bits_of_m(uint32_t x) { return ((x << 4 ^ x >> 12) & 0xffff0u) + 8u; }
+__device__ __forceinline__ uint32_t bits_of_root(uint32_t x) { return (x >> 12 & 0xffff0u) + 8u; }
 
 // Power of two that brings `largest` into [128, 256), at least 2^-107; and its reciprocal.
 __device__ __forceinline__ float2 scale_of(float largest)
@@ -387,7 +392,7 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
-        const uint32_t x = mix(first + k * GOLDEN), y = mix(first + (k + 1) * GOLDEN);
+        const uint32_t x = mix_but_for_the_last(first + k * GOLDEN), y = mix_but_for_the_last(first + (k + 1) * GOLDEN);
         // the sign stays where it is: adding below it does not carry into it
         m[k] = __uint_as_float((__float_as_uint(a.x) + bits_of_m(x)) & 0xfff00000u);
         m[k + 1] = __uint_as_float((__float_as_uint(a.y) + bits_of_m(y)) & 0xfff00000u);
@@ -409,7 +414,7 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
 }
 
 // KINDS: which states the list has, 1 in 32 bits, 2 in 8 bits, 3 both (with the registers of the larger).  8-bit states
-// alone are best with five blocks to an SM and 48 registers: 238 us, with four 251, with six, which spill, 262.
+// alone are best with five blocks to an SM and 48 registers: with four they take 5 % longer, with six, which spill, 10 %.
 template <int N, int KINDS>
 __global__ void __launch_bounds__(AW_THREADS, KINDS == 2 ? 5 : 4) adamw_kernel(const __grid_constant__ Table<N> table)
 {
