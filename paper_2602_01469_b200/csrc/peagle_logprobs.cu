@@ -10,11 +10,11 @@
 //
 // The floor is one read.  A block takes a row in chunks of 16 bytes per thread and load, the next chunk on its way.  Few
 // rows are cut into parts for a cluster of up to 16 blocks, which join through distributed shared memory.  4,096 rows of
-// 128,000 bf16 take 200 us without alternatives (80 % of the copy rate), 240 with 8 (67 %), 268 with 20; 2,048 rows of
-// fp32, the same bytes, 198 with 8 (81 %).  Nothing is full (1,184 rows: issue slots 61 % without alternatives, 69 with,
+// 128,000 bf16 take 200 us without alternatives (80 % of the copy rate), 233 with 8 (69 %), 255 with 20; 2,048 rows of
+// fp32, the same bytes, 193 with 8 (83 %).  Nothing is full (1,184 rows: issue slots 61 % without alternatives, 69 with,
 // 8 and 11 instructions per entry, exp2 unit 50 %): a chunk's steps depend on each other, and the 32 warps of an SM
-// do not cover that.  With c, low and the sums kept as pairs from chunk to chunk there are fewer instructions, the
-// registers spill, and it takes 260.
+// do not cover that.  The next chunk but one is sent for as soon as a chunk's pieces are in registers and what of them
+// reaches the list is there; after the sums it took 241 with 8 and 265 with 20.
 //
 // Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
 // k-th largest of the maxima of 64 groups of threads, then the k-th best entry so far).  A chunk's maximum, which the
@@ -400,6 +400,61 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                 all = max_words<T>(all, most[u]);
             }
             const float top = of_max_word<T>(all);
+            const auto offer = [&](float v, int id, uint64_t least) {
+                const uint64_t key = rank_key(v, begin + id);
+                if (id >= 0 && id < n && key >= least) {
+                    const int place = atomicAdd(&count, 1);
+                    if (place < LIST)
+                        list[place] = key;
+                    end = place + 1;
+                }
+            };
+            if constexpr (TOP) {
+                const int k = a.top_k;
+                if (first == 0) { // the k-th largest of the maxima of 64 groups of threads
+                    constexpr int LANES = LP_THREADS / GROUPS;
+                    float most = top;
+#pragma unroll
+                    for (int o = 1; o < LANES; o *= 2)
+                        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+                    if (threadIdx.x % LANES == 0)
+                        reinterpret_cast<float *>(first_max)[threadIdx.x / LANES] = most;
+                    __syncthreads();
+                    if (threadIdx.x < GROUPS) {
+                        most = reinterpret_cast<float *>(first_max)[threadIdx.x];
+                        int above = 0, equal = 0;
+#pragma unroll
+                        for (int i = 0; i < GROUPS / 4; ++i) {
+                            const float4 o = first_max[i];
+                            above += (o.x > most) + (o.y > most) + (o.z > most) + (o.w > most);
+                            equal += (o.x == most) + (o.y == most) + (o.z == most) + (o.w == most);
+                        }
+                        if (above < k && above + equal >= k)
+                            first_bound = most;
+                    }
+                    __syncthreads();
+                    bound = first_bound;
+                }
+                if (top >= bound) {
+                    // which of the entries reach the bound, without a branch among a piece's: a thread on this path
+                    // keeps its whole block waiting
+                    uint32_t reach = 0;
+#pragma unroll
+                    for (int u = 0; u < U; ++u)
+                        if (of_max_word<T>(most[u]) >= bound) {
+#pragma unroll
+                            for (int e = 0; e < N; ++e)
+                                reach |= (uint32_t)(now[u].get(e) >= bound) << (u * N + e);
+                        }
+                    for (; reach; reach &= reach - 1) {
+                        const int i = __ffs(reach) - 1, u = i / N, e = i % N;
+                        offer(to_f32(reinterpret_cast<const T *>(at + u * LP_THREADS)[e]),
+                              (first + u * LP_THREADS + (int)threadIdx.x) * N + e - before, 0);
+                    }
+                }
+            }
+            fetch(first + STAGES * STEP, stage); // into the places of this chunk, which the thread has in registers
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
             if (top > s.m)
                 rescale(s, top, l);
             const float c = reference(s.m, l);
@@ -439,9 +494,10 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
 #pragma unroll 1
                     for (int i = 0; i < U * N; ++i) {
                         const int id = (first + i / N * LP_THREADS + (int)threadIdx.x) * N + i % N - before;
-                        const float t = fmaf(to_f32(reinterpret_cast<const T *>(at + i / N * LP_THREADS)[i % N]), l, -c);
-                        if (id >= 0 && id < n)
-                            s.E = fmaf(fast_exp2(t), fmaxf(t, T_FLOOR), s.E);
+                        if (id < 0 || id >= n)
+                            continue;
+                        const float t = fmaf(to_f32(row[begin + id]), l, -c);
+                        s.E = fmaf(fast_exp2(t), fmaxf(t, T_FLOOR), s.E);
                     }
                 } else {
                     s.E = E;
@@ -451,58 +507,7 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
             }
             if constexpr (TOP) {
                 const int k = a.top_k;
-                if (first == 0) { // the k-th largest of the maxima of 64 groups of threads
-                    constexpr int LANES = LP_THREADS / GROUPS;
-                    float most = top;
-#pragma unroll
-                    for (int o = 1; o < LANES; o *= 2)
-                        most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
-                    if (threadIdx.x % LANES == 0)
-                        reinterpret_cast<float *>(first_max)[threadIdx.x / LANES] = most;
-                    __syncthreads();
-                    if (threadIdx.x < GROUPS) {
-                        most = reinterpret_cast<float *>(first_max)[threadIdx.x];
-                        int above = 0, equal = 0;
-#pragma unroll
-                        for (int i = 0; i < GROUPS / 4; ++i) {
-                            const float4 o = first_max[i];
-                            above += (o.x > most) + (o.y > most) + (o.z > most) + (o.w > most);
-                            equal += (o.x == most) + (o.y == most) + (o.z == most) + (o.w == most);
-                        }
-                        if (above < k && above + equal >= k)
-                            first_bound = most;
-                    }
-                    __syncthreads();
-                    bound = first_bound;
-                }
-                uint64_t least = 0;
                 while (true) {
-                    if (top >= bound) {
-                        // which of the entries reach the bound, without a branch among a piece's: a thread on this path
-                        // keeps its whole block waiting
-                        uint32_t reach = 0;
-#pragma unroll
-                        for (int u = 0; u < U; ++u)
-                            if (of_max_word<T>(most[u]) >= bound) {
-                                Piece<T> p;
-                                p.v = at[u * LP_THREADS];
-#pragma unroll
-                                for (int e = 0; e < N; ++e)
-                                    reach |= (uint32_t)(p.get(e) >= bound) << (u * N + e);
-                            }
-                        for (; reach; reach &= reach - 1) {
-                            const int i = __ffs(reach) - 1, u = i / N, e = i % N;
-                            const int id = (first + u * LP_THREADS + (int)threadIdx.x) * N + e - before;
-                            const float v = to_f32(reinterpret_cast<const T *>(at + u * LP_THREADS)[e]);
-                            const uint64_t key = rank_key(v, begin + id);
-                            if (id >= 0 && id < n && key >= least) {
-                                const int place = atomicAdd(&count, 1);
-                                if (place < LIST)
-                                    list[place] = key;
-                                end = place + 1;
-                            }
-                        }
-                    }
                     const bool meet = first / STEP % every == every - 1;
                     if (!meet || !__syncthreads_or(end > long_list)) {
                         if (meet)
@@ -525,7 +530,7 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                         break;
                     }
                     // once more, for what reaches the k-th best of those that found a place
-                    least = kth_best(list, LIST, k);
+                    const uint64_t least = kth_best(list, LIST, k);
                     uint64_t mine[LIST / LP_THREADS];
 #pragma unroll
                     for (int j = 0; j < LIST / LP_THREADS; ++j)
@@ -540,12 +545,19 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                         if (mine[j] >= least && (int)~(uint32_t)mine[j] < chunk_id) // from the chunks before
                             list[atomicAdd(&count, 1)] = mine[j];
                     bound = from_key((uint32_t)(least >> 32));
+#pragma unroll 1
+                    for (int i = 0; i < U * N; ++i) {
+                        const int id = (first + i / N * LP_THREADS + (int)threadIdx.x) * N + i % N - before;
+                        if (id >= 0 && id < n) {
+                            const float v = to_f32(row[begin + id]);
+                            if (v >= bound)
+                                offer(v, id, least);
+                        }
+                    }
                 }
             }
             if (TOP && overflow)
                 break;
-            fetch(first + STAGES * STEP, stage);
-            stage = stage + 1 == STAGES ? 0 : stage + 1;
         }
         if (!TOP)
             break;
