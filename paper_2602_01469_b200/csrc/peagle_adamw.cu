@@ -13,16 +13,17 @@
 // so scaling is exact and the rounding to a code looks at the fp32 number's own bits: adding 20 random bits below
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
-// bounds this is instructions, about 70 per element and half of them integer ones for the random bits and the
-// roundings: 91 M elements, bf16, take 229 us, 61 % of the copy rate.  A first version had 113 and took 343; it formed
-// the new m and v in fp64 so that the codes would not depend on how the arithmetic is ordered.  In fp32 two or three
-// codes in a million fall on the other side of the random bits, which is as good a rounding; only a block's scale has
-// to be right, and where a block's largest number lies at a power of two, or is not finite, the largest is found
-// again in fp64.  (Blocks that stay, with the next chunk on its way in shared memory, have more instructions: 260.)
+// bounds this is instructions, more than half of them integer ones for the random bits and the roundings: 91 M elements,
+// bf16, take 262 us, 54 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, 229, two or three
+// codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
+// a code whose number is near its border, and the largest number of a block near a power of two, are formed again in
+// fp64, and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
+// more instructions: 260 where this way took 254.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
 #include <cmath>
+#include <cstring>
 
 #include "peagle_internal.h"
 #include "sm100_ptx.cuh"
@@ -61,6 +62,7 @@ struct Factors {
 struct How {
     double beta1, beta2;
     float eps;
+    float b1_top, b1_rest, c1, c1_rest, b2, c2; // beta1 in two parts, 1 - beta1 in two, beta2, 1 - beta2
     uint32_t seed, ordinal; // place of the first tensor in the caller's list
     uint32_t chunks;
     int n;
@@ -210,18 +212,35 @@ __device__ __forceinline__ uint32_t encode4(float a, float b, float c, float d)
     return (uint32_t)hi << 16 | lo;
 }
 
-// y rounded up or down by 20 random bits, where the plain way (`large`) does not do: below 2^-6, where e4m3's spacing is
-// even, and not finite.  `keep`: above zero stays above it.
-__device__ __forceinline__ float small_code(float y, float large, uint32_t bits20, bool keep)
+// A number within NEAR units in the last place of the border between two codes, the random bits added, is rounded again
+// from fp64: see nearness.
+constexpr uint32_t NEAR = 8;
+// y rounded up or down by 20 random bits.  What is left over tells how near the border is.
+__device__ __forceinline__ float rounded(float y, uint32_t bits20, uint32_t &nearness)
+{
+    const uint32_t z = __float_as_uint(y) + bits20 + NEAR; // the sign stays: adding below it does not carry into it
+    nearness = min(nearness, z & 0xfffffu);                // less than 2 NEAR: too near, else NEAR changes nothing
+    return __uint_as_float(z & 0xfff00000u);
+}
+// The same where the plain way (`large`) does not do: below 2^-6, where e4m3's spacing is even, and not finite.  `keep`:
+// above zero stays above it.
+__device__ __forceinline__ float small_code(float y, float large, uint32_t bits20, bool keep, uint32_t &nearness)
 {
     const float a = fabsf(y);
     if (a >= 0.015625f)
         return a <= 256.f ? large : __int_as_float(0x7fffffff);
-    const float z = __uint_as_float((__float_as_uint(a + 0.015625f) + bits20) & 0xfff00000u) - 0.015625f;
+    const float z = rounded(a + 0.015625f, bits20, nearness) - 0.015625f;
     return a != a ? a : copysignf(keep && a > 0.f ? fmaxf(z, 0.001953125f) : z, y); // 2^-9
 }
+// The code of a number that is exact.
+__device__ __forceinline__ uint32_t exact_code(float y, uint32_t bits20, bool keep)
+{
+    uint32_t none = 0;
+    const uint32_t less = bits20 - NEAR; // rounded() adds it
+    return encode4(small_code(y, rounded(y, less, none), less, keep, none), 0.f, 0.f, 0.f) & 0xffu;
+}
 // The 20 bits of an element for m and for the root: the lower and the upper 16 of mix(), and a half.  From what mix()
-// has before its last step, which leaves the upper ones as they are: 91 M elements 229 us, from mix() itself 238.
+// has before its last step, which leaves the upper ones as they are: 4 % faster than from mix() itself.
 __device__ __forceinline__ uint32_t bits_of_m(uint32_t x) { return ((x << 4 ^ x >> 12) & 0xffff0u) + 8u; }
 __device__ __forceinline__ uint32_t bits_of_root(uint32_t x) { return (x >> 12 & 0xffff0u) + 8u; }
 
@@ -232,7 +251,7 @@ __device__ __forceinline__ float2 scale_of(float largest)
     return make_float2(__uint_as_float((uint32_t)(e + 127) << 23), __uint_as_float((uint32_t)(127 - e) << 23));
 }
 
-__device__ __forceinline__ F2 both(double x) { return f2((float)x, (float)x); }
+__device__ __forceinline__ F2 both(float x) { return f2(x, x); }
 __device__ __forceinline__ void put2(float (&to)[8], int k, F2 v)
 {
     const float2 u = unf2(v);
@@ -294,7 +313,7 @@ __device__ __forceinline__ void step8(const Tensor &t, const How &how, const Fac
     load8<VEC>(t.grad, t.grad_dtype, i, left, g);
     load8<VEC>(t.master ? t.master : t.param, t.master ? PEAGLE_F32 : t.param_dtype, i, left, p);
     const float decay = -f.lr * t.weight_decay;
-    const F2 b1 = both(how.beta1), c1 = both(1.0 - how.beta1), b2 = both(how.beta2), c2 = both(1.0 - how.beta2);
+    const F2 b1 = both(how.b1_top + how.b1_rest), c1 = both(how.c1), b2 = both(how.b2), c2 = both(how.c2);
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
@@ -319,21 +338,50 @@ __device__ __forceinline__ void exact_states(const How &how, float m0, float r0,
     root = __fsqrt_rn((float)__dadd_rn(__dmul_rn(how.beta2, (double)(r0 * r0)), __dmul_rn(__dmul_rn(1.0 - how.beta2, gd), gd)));
 }
 
+// What one element has in memory, and its new m and root.
+__device__ __forceinline__ void exact_element(const Tensor &t, const How &how, float grad_scale, int64_t i, float &m, float &root)
+{
+    const float ms = t.m_scale[i / AW_BLOCK], vs = t.v_scale[i / AW_BLOCK];
+    const float g = t.grad_dtype == PEAGLE_F32 ? static_cast<const float *>(t.grad)[i]
+                                               : __bfloat162float(static_cast<const __nv_bfloat16 *>(t.grad)[i]);
+    float m0[8], r0[8];
+    decode4(static_cast<const uint8_t *>(t.m)[i], m0, 0);
+    decode4(static_cast<const uint8_t *>(t.v)[i], r0, 0);
+    exact_states(how, m0[0] * ms, r0[0] * vs, g * grad_scale, m, root);
+}
+
+// A thread's codes from fp64, where one of them was too near a border.  From memory, like the next.
+__device__ __forceinline__ void exact_codes(const Tensor &t, const How &how, float grad_scale, int64_t i, int left, uint32_t first,
+                                            float m_factor, float r_factor, uint2 &m_codes, uint2 &r_codes)
+{
+#pragma unroll 1
+    for (int k = 0; k < left; ++k) {
+        float m, r;
+        exact_element(t, how, grad_scale, i + k, m, r);
+        const uint32_t x = mix_but_for_the_last(first + k * GOLDEN), at = k % 4 * 8, keep = ~(0xffu << at);
+        const uint32_t mc = exact_code(m * m_factor, bits_of_m(x), false) << at;
+        const uint32_t rc = exact_code(r * r_factor, bits_of_root(x), true) << at;
+        if (k < 4) {
+            m_codes.x = m_codes.x & keep | mc;
+            r_codes.x = r_codes.x & keep | rc;
+        } else {
+            m_codes.y = m_codes.y & keep | mc;
+            r_codes.y = r_codes.y & keep | rc;
+        }
+    }
+}
+
 // Largest magnitudes of a doubtful block, without the elements that are not finite.  From memory: the numbers that the
 // caller has are not kept for this rare case.
 __device__ __forceinline__ void exact_largest(const Tensor &t, const How &how, float grad_scale, int64_t i, int left,
                                               uint32_t &largest_m, uint32_t &largest_r)
 {
-    const float ms = t.m_scale[i / AW_BLOCK], vs = t.v_scale[i / AW_BLOCK];
     uint32_t lm = 0, lr = 0;
 #pragma unroll 1
     for (int k = 0; k < left; ++k) {
-        float m[8], r[8], g = t.grad_dtype == PEAGLE_F32 ? static_cast<const float *>(t.grad)[i + k]
-                                                         : __bfloat162float(static_cast<const __nv_bfloat16 *>(t.grad)[i + k]);
-        decode4(static_cast<const uint8_t *>(t.m)[i + k], m, 0);
-        decode4(static_cast<const uint8_t *>(t.v)[i + k], r, 0);
-        exact_states(how, m[0] * ms, r[0] * vs, g * grad_scale, m[0], r[0]);
-        const uint32_t mb = __float_as_uint(fabsf(m[0])), rb = __float_as_uint(fabsf(r[0]));
+        float m, r;
+        exact_element(t, how, grad_scale, i + k, m, r);
+        const uint32_t mb = __float_as_uint(fabsf(m)), rb = __float_as_uint(fabsf(r));
         lm = mb < 0x7f800000u ? max(lm, mb) : lm;
         lr = rb < 0x7f800000u ? max(lr, rb) : lr;
     }
@@ -357,13 +405,16 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     decode4(mc.y, m, 4);
     decode4(vc.x, r, 0);
     decode4(vc.y, r, 4);
-    const float decay = -f.lr * t.weight_decay, b1s = (float)how.beta1 * ms; // by a power of two: exact
-    const F2 b1 = f2(b1s, b1s), c1 = both(1.0 - how.beta1), b2 = both(how.beta2), c2 = both(1.0 - how.beta2), vs2 = f2(vs, vs);
+    const float decay = -f.lr * t.weight_decay, b1s = how.b1_top * ms, b1r = how.b1_rest * ms; // by a power of two: exact
+    const F2 b1 = both(b1s), b1_rest = both(b1r), c1 = both(how.c1), c1_rest = both(how.c1_rest), b2 = both(how.b2),
+             c2 = both(how.c2), vs2 = both(vs);
     float m_max = 0.f, r_max = 0.f, m_min = 1e38f, r_min = 1e38f;
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
-        const F2 m2 = fma_f2(b1, f2(m[k], m[k + 1]), mul_f2(c1, gg));
+        // b1_top's product with a code is exact, so whatever cancels, m is right to two units in the last place
+        const F2 code = f2(m[k], m[k + 1]), rest = fma_f2(c1_rest, gg, mul_f2(b1_rest, code));
+        const F2 m2 = add_f2(fma_f2(c1, gg, mul_f2(b1, code)), rest);
         const F2 r0 = mul_f2(f2(r[k], r[k + 1]), vs2);
         const float2 v = unf2(fma_f2(b2, mul_f2(r0, r0), mul_f2(mul_f2(c2, gg), gg)));
         put2(m, k, m2);
@@ -389,24 +440,29 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     const uint32_t first = key + (uint32_t)i * GOLDEN;
     const bool plain = finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f;
     const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
+    uint32_t nearness = ~0u;
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
         const uint32_t x = mix_but_for_the_last(first + k * GOLDEN), y = mix_but_for_the_last(first + (k + 1) * GOLDEN);
-        // the sign stays where it is: adding below it does not carry into it
-        m[k] = __uint_as_float((__float_as_uint(a.x) + bits_of_m(x)) & 0xfff00000u);
-        m[k + 1] = __uint_as_float((__float_as_uint(a.y) + bits_of_m(y)) & 0xfff00000u);
-        r[k] = __uint_as_float((__float_as_uint(b.x) + bits_of_root(x)) & 0xfff00000u);
-        r[k + 1] = __uint_as_float((__float_as_uint(b.y) + bits_of_root(y)) & 0xfff00000u);
+        m[k] = rounded(a.x, bits_of_m(x), nearness);
+        m[k + 1] = rounded(a.y, bits_of_m(y), nearness);
+        r[k] = rounded(b.x, bits_of_root(x), nearness);
+        r[k + 1] = rounded(b.y, bits_of_root(y), nearness);
         if (!plain) { // small numbers, roots that must not become zero, and what is not finite
-            m[k] = small_code(a.x, m[k], bits_of_m(x), false);
-            m[k + 1] = small_code(a.y, m[k + 1], bits_of_m(y), false);
-            r[k] = small_code(b.x, r[k], bits_of_root(x), true);
-            r[k + 1] = small_code(b.y, r[k + 1], bits_of_root(y), true);
+            m[k] = small_code(a.x, m[k], bits_of_m(x), false, nearness);
+            m[k + 1] = small_code(a.y, m[k + 1], bits_of_m(y), false, nearness);
+            r[k] = small_code(b.x, r[k], bits_of_root(x), true, nearness);
+            r[k + 1] = small_code(b.y, r[k + 1], bits_of_root(y), true, nearness);
         }
     }
-    store_codes<VEC>(t.m, i, left, make_uint2(encode4(m[0], m[1], m[2], m[3]), encode4(m[4], m[5], m[6], m[7])));
-    store_codes<VEC>(t.v, i, left, make_uint2(encode4(r[0], r[1], r[2], r[3]), encode4(r[4], r[5], r[6], r[7])));
+    uint2 m_codes = make_uint2(encode4(m[0], m[1], m[2], m[3]), encode4(m[4], m[5], m[6], m[7]));
+    uint2 r_codes = make_uint2(encode4(r[0], r[1], r[2], r[3]), encode4(r[4], r[5], r[6], r[7]));
+    if (nearness < 2 * NEAR)
+        exact_codes(t, how, grad_scale, i, left, first, sm.y, sv.y, m_codes, r_codes);
+    store_codes<VEC>(t.m, i, left, m_codes);
+    store_codes<VEC>(t.v, i, left, r_codes);
+    __syncwarp(); // nobody reads the old scales any more
     if (threadIdx.x % 32 == 0) {
         t.m_scale[block] = sm.x;
         t.v_scale[block] = sv.x;
@@ -486,6 +542,16 @@ int launch_adamw(const peagle_adamw_t &how, const peagle_adamw_tensor_t *tensors
     How h = {};
     h.beta1 = how.beta1;
     h.beta2 = how.beta2;
+    const float b1 = (float)how.beta1;
+    uint32_t top;
+    std::memcpy(&top, &b1, 4);
+    top &= 0xffffff00u; // 16 significant bits: the product with a code's 4 is exact
+    std::memcpy(&h.b1_top, &top, 4);
+    h.b1_rest = (float)(how.beta1 - (double)h.b1_top);
+    h.c1 = (float)(1.0 - how.beta1);
+    h.c1_rest = (float)(1.0 - how.beta1 - (double)h.c1);
+    h.b2 = (float)how.beta2;
+    h.c2 = (float)(1.0 - how.beta2);
     h.log_beta1 = std::log(how.beta1);
     h.log_beta2 = std::log(how.beta2);
     h.lr = (float)how.lr;
