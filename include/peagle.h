@@ -397,7 +397,7 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
  * the probability of the fraction, because to the nearest an average with beta2 near 1 would never move: its steps
  * are smaller than half a code.  (A root above zero is never stored as zero, it divides the next step.)  The random
  * bits are a hash of (seed, step, place of the tensor in the list, element), so a step repeats bit for bit.  The new
- * m and root are fp32 before they are rounded.  An element whose new state is not finite is stored as NaN and does not
+ * m and v are as from fp64, rounded to fp32 once, and the root is fp32's, before codes are taken.  An element whose new state is not finite is stored as NaN and does not
  * count for its block's scale.  All zero codes and any finite scales are the states to begin with.
  * lr_dev, step_dev, grad_scale_dev (dev, each may be NULL) replace lr, step and the factor 1, so that a captured
  * graph can be replayed with others.  lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0, step >= 1 (not checked on

@@ -14,7 +14,7 @@
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, more than half of them integer ones for the random bits and the roundings: 91 M elements,
-// bf16, take 262 us, 54 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, 229, two or three
+// bf16, take 248 us, 57 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, 229, two or three
 // codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
 // a code whose number is near its border, and the largest number of a block near a power of two, are formed again in
 // fp64, and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
@@ -219,7 +219,7 @@ constexpr uint32_t NEAR = 8;
 __device__ __forceinline__ float rounded(float y, uint32_t bits20, uint32_t &nearness)
 {
     const uint32_t z = __float_as_uint(y) + bits20 + NEAR; // the sign stays: adding below it does not carry into it
-    nearness = min(nearness, z & 0xfffffu);                // less than 2 NEAR: too near, else NEAR changes nothing
+    nearness = min(nearness, z << 12);                     // less than 2 NEAR << 12: too near, else NEAR changes nothing
     return __uint_as_float(z & 0xfff00000u);
 }
 // The same where the plain way (`large`) does not do: below 2^-6, where e4m3's spacing is even, and not finite.  `keep`:
@@ -458,7 +458,7 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     }
     uint2 m_codes = make_uint2(encode4(m[0], m[1], m[2], m[3]), encode4(m[4], m[5], m[6], m[7]));
     uint2 r_codes = make_uint2(encode4(r[0], r[1], r[2], r[3]), encode4(r[4], r[5], r[6], r[7]));
-    if (nearness < 2 * NEAR)
+    if (nearness < 2 * NEAR << 12)
         exact_codes(t, how, grad_scale, i, left, first, sm.y, sv.y, m_codes, r_codes);
     store_codes<VEC>(t.m, i, left, m_codes);
     store_codes<VEC>(t.v, i, left, r_codes);

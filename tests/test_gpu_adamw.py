@@ -162,6 +162,26 @@ def test_a_large_tensor(ctx, bits):
     check(before, item, 0, 4, 9)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_every_code_is_the_defined_one(ctx, dtype):
+    """m and v as from fp64, rounded to fp32 once: also where a number lies next to the border of its code, and a step
+    later, when a code on the other side would have moved its block's scale."""
+    gen = torch.Generator().manual_seed(12)
+    item = make(gen, 1_500_003, dtype, dtype, 8, False, 0.1)
+    tensors = binding.AdamWTensors([item])
+    code = lambda t: t.view(torch.uint8).cpu().numpy().ravel()
+    for step in (3, 4):
+        b = snapshot(item)
+        binding.peagle_adamw_step(ctx, tensors, step=step, seed=5, **HOW)
+        torch.cuda.synchronize()
+        _, _, mc, vc, _, _, ms, vs = oo.adamw_states8(f64(b["grad"]).ravel(), code(b["m"]), code(b["v"]), f64(b["m_scale"]),
+                                                      f64(b["v_scale"]), HOW["beta1"], HOW["beta2"], 5, step, 0)
+        assert np.array_equal(f64(item["m_scale"]), ms) and np.array_equal(f64(item["v_scale"]), vs)
+        values = oo.e4m3_values()
+        for name, want in (("m", mc), ("v", vc)):
+            assert np.array_equal(values[code(item[name])], values[want], equal_nan=True), name
+
+
 def test_states_that_begin_at_zero(ctx):
     gen = torch.Generator().manual_seed(7)
     item = make(gen, 700, F32, F32, 8, False, 0.0)
