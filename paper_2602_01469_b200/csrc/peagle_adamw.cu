@@ -412,7 +412,8 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
-        // b1_top's product with a code is exact, so whatever cancels, m is right to two units in the last place
+        // b1_top's product with a code is exact and the rest is 2^-16 of it, so m is right to a few units in the last
+        // place where up to 2^19 of its terms cancels; what is smaller is far below a code's spacing
         const F2 code = f2(m[k], m[k + 1]), rest = fma_f2(c1_rest, gg, mul_f2(b1_rest, code));
         const F2 m2 = add_f2(fma_f2(c1, gg, mul_f2(b1, code)), rest);
         const F2 r0 = mul_f2(f2(r[k], r[k + 1]), vs2);
