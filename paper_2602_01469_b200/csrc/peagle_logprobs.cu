@@ -544,6 +544,7 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
                     for (int j = 0; j < LIST / LP_THREADS; ++j)
                         if (mine[j] >= least && (int)~(uint32_t)mine[j] < chunk_id) // from the chunks before
                             list[atomicAdd(&count, 1)] = mine[j];
+                    __syncthreads(); // these, k at most, have their places before the chunk's entries take theirs
                     bound = from_key((uint32_t)(least >> 32));
 #pragma unroll 1
                     for (int i = 0; i < U * N; ++i) {

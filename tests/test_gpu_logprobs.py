@@ -225,6 +225,28 @@ def test_rows_that_overflow_the_list_late(ctx, dtype, repeat):
     check_forward(x, tokens, 0.9, k, forward(ctx, x, tokens, 0.9, k))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("k", [20, 64])
+@pytest.mark.parametrize("repeat", [1, 50]) # rows cut into parts, and whole ones
+def test_early_best_entries_survive_a_late_overflow(ctx, dtype, k, repeat):
+    """Some of the k best come first and an ascending tail follows, which fills the list several times over within a
+    chunk: the early ones are put back into the list while the chunk is gone through again."""
+    vocab = 20011
+    gen = torch.Generator().manual_seed(15)
+    rows = []
+    for early in (1, k // 2, k - 1, k):
+        for at in (4096, 9000, 16500):
+            r = torch.randn(vocab, generator=gen)
+            r[at:] = torch.linspace(8, 40, vocab - at)
+            where = torch.randperm(min(at, 4096), generator=gen)[:early]
+            r[where] = 64.0 + 2.0 * torch.arange(early)
+            rows.append(r)
+    x = torch.stack(rows).repeat(repeat, 1).to(dtype)
+    tokens = torch.randint(-1, vocab, (x.shape[0],), generator=gen).to(torch.int32).to(DEV)
+    x = put(x, 0, 0)
+    check_forward(x, tokens, 1.0, k, forward(ctx, x, tokens, 1.0, k))
+
+
 def test_a_peaked_row_keeps_its_digits(ctx):
     """Large logits and a probability near one: neither logprob nor 1 - p is a difference of rounded numbers."""
     x = torch.full((2, 5000), 20.0)
