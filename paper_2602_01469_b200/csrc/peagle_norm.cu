@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
 
 // LAYER: layer norm, else RMS norm.  SUMS: 1 of dy xh (dw), 2 of dy too (db).  With z = x - mu the products are
 // arranged for few operations per element: t = dy z gives sum u xh = rstd sum t w and dw += rstd t, and
-// dx = rstd w dy + (-rstd^2 mean(u xh)) z - rstd mean(u).
+// dx = rstd (w dy - mean(u) + (-rstd mean(u xh)) z).
 template <class T, bool VEC, bool LAYER, int TPR, int E, int SUMS>
 __global__ void __launch_bounds__(block_threads(TPR),
                                   blocks_per_sm(block_threads(TPR), 2 * Part<T, VEC, TPR, E>::WORDS + SUMS * E))
@@ -476,7 +476,8 @@ __global__ void __launch_bounds__(block_threads(TPR),
         copies_commit();
         if (D > 1)
             stage ^= 1;
-        const float c0 = -rs * per_col * s.x, c1 = -rs * rs * rs * per_col * s.y;
+        // from left to right: the mean of u xh has the size of u, while rstd^3 alone leaves fp32's range for rows of 1e13
+        const float c0 = -s.x * per_col, c1 = -(rs * s.y * per_col) * rs;
         x.forget();
         dy.forget();
 #pragma unroll
@@ -485,9 +486,9 @@ __global__ void __launch_bounds__(block_threads(TPR),
             Row::weights4(sw, t, e, w[0], w[1]);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-                const F2 x2 = x.get2(e + 2 * k);
-                const F2 rest = LAYER ? fma_f2(add_f2(x2, minus), f2(c1, c1), f2(c0, c0)) : mul_f2(x2, f2(c1, c1));
-                x.set2(e + 2 * k, fma_f2(dy.get2(e + 2 * k), mul_f2(w[k], by), rest));
+                const F2 x2 = x.get2(e + 2 * k), z = LAYER ? add_f2(x2, minus) : x2, d = dy.get2(e + 2 * k);
+                const F2 u = LAYER ? fma_f2(d, w[k], f2(c0, c0)) : mul_f2(d, w[k]);
+                x.set2(e + 2 * k, mul_f2(fma_f2(z, f2(c1, c1), u), by));
             }
         }
         if (r < rows)

@@ -180,6 +180,26 @@ def test_a_mean_far_from_zero_and_a_constant_row(ctx):
     assert float(y[3].abs().max()) == 0.0
 
 
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [72, 1001, 2880, 18000])
+def test_rows_of_very_large_and_very_small_numbers(ctx, kind, dtype, cols):
+    """The cube of rstd is no fp32 number for rows of 1e13 and larger, nor for rows of zeros with a tiny eps."""
+    gen = torch.Generator().manual_seed(cols)
+    w = (1 + 0.3 * torch.randn(cols, generator=gen)).to(dtype).to(DEV)
+    size = torch.tensor([1e-14, 0.0, 1e-6, 1.0, 1e8, 1e12, 1e13, 3e13, 1e14, 1e15, 1e16, 1e17])
+    x = (torch.randn(len(size), cols, generator=gen) * size[:, None]).to(dtype).to(DEV)
+    dy = torch.randn(len(size), cols, generator=gen).to(dtype).to(DEV)
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(len(size), device=DEV), torch.empty(len(size), device=DEV)
+    binding.peagle_norm_fwd(ctx, binding.NORM[kind], x, w, None, 1e-30, y, mean, rstd)
+    check_fwd(kind, x, w, None, float(np.float32(1e-30)), y, mean, rstd)
+    m = mean if kind == "layer" else None
+    dw, db, zero = torch.zeros(cols, device=DEV), torch.zeros(cols, device=DEV), torch.zeros(cols, device=DEV)
+    binding.peagle_norm_bwd(ctx, binding.NORM[kind], x, w, m, rstd, dy, dx, dw, db)
+    check_bwd(kind, x, w, m, rstd, dy, dx, dw, zero, db, zero)
+
+
 def test_nan_and_infinity_stay_in_their_rows(ctx):
     gen = torch.Generator().manual_seed(6)
     for cols in (128, 2880, 1001):
