@@ -400,9 +400,10 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
  * m and v are as from fp64, rounded to fp32 once, and the root is fp32's, before codes are taken.  An element whose new state is not finite is stored as NaN and does not
  * count for its block's scale.  All zero codes and any finite scales are the states to begin with.
  * lr_dev, step_dev, grad_scale_dev (dev, each may be NULL) replace lr, step and the factor 1, so that a captured
- * graph can be replayed with others.  lr >= 0, 0 <= beta < 1, eps > 0, weight_decay >= 0, step >= 1 (not checked on
- * the device).  Tensors must not share memory.  `tensors` is a host array, read before the call returns; a launch
- * takes PEAGLE_ADAMW_TENSORS of them.  Asynchronous; nothing is allocated.
+ * graph can be replayed with others.  lr >= 0, 0 <= beta < 1, weight_decay >= 0, step >= 1 (not checked on the device);
+ * eps >= 2^-126, fp32's smallest normal number: the step is taken in fp32, where a smaller one could count as zero and
+ * an element with m = v = 0 become 0 / 0.  Tensors must not share memory.  `tensors` is a host array, read before the
+ * call returns; a launch takes PEAGLE_ADAMW_TENSORS of them.  Asynchronous; nothing is allocated.
  */
 #define PEAGLE_ADAMW_BLOCK 256
 #define PEAGLE_ADAMW_TENSORS 384

@@ -1,5 +1,6 @@
 // C ABI of libpeagle: context, argument validation, scratch memory, and the drivers that chain
 // K0 (mask evaluator / tile classifier / scheduler), K1 (forward) and K2 (backward).
+#include <float.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -1456,7 +1457,7 @@ int peagle_adamw_step(peagle_ctx *ctx, const peagle_adamw_t *how, const peagle_a
         return PEAGLE_ERR_NULL;
     const double huge = 1e30;
     if (n_tensors < 0 || !(how->lr >= 0.0 && how->lr <= huge) || !(how->beta1 >= 0.0 && how->beta1 < 1.0) ||
-        !(how->beta2 >= 0.0 && how->beta2 < 1.0) || !(how->eps > 0.0 && how->eps <= huge) ||
+        !(how->beta2 >= 0.0 && how->beta2 < 1.0) || !(how->eps >= FLT_MIN && how->eps <= huge) ||
         (!how->step_dev && how->step < 1))
         return PEAGLE_ERR_BAD_SHAPE;
     if (!aligned_to(how->lr_dev, 4) || !aligned_to(how->step_dev, 8) || !aligned_to(how->grad_scale_dev, 4))

@@ -182,6 +182,21 @@ def test_every_code_is_the_defined_one(ctx, dtype):
             assert np.array_equal(values[code(item[name])], values[want], equal_nan=True), name
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+def test_untouched_elements_stay_with_the_smallest_eps(ctx, bits):
+    """m = v = g = 0, a row of an embedding that no token has met: the step is 0 / eps = 0, the decay remains."""
+    gen = torch.Generator().manual_seed(13)
+    item = make(gen, 3000, F32, F32, bits, False, 0.1, offset=1)
+    for name in ("m", "v"):
+        item[name].view(torch.uint8 if bits == 8 else F32).zero_()
+    item["grad"].zero_()
+    how = dict(lr=3e-3, beta1=0.9, beta2=0.98, eps=2.0 ** -126)
+    before = snapshot(item)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors([item]), step=1, seed=2, **how)
+    torch.cuda.synchronize()
+    check(before, item, 0, 1, 2, how)
+
+
 def test_states_that_begin_at_zero(ctx):
     gen = torch.Generator().manual_seed(7)
     item = make(gen, 700, F32, F32, 8, False, 0.0)

@@ -279,6 +279,13 @@ def test_adamw_refusals(lib, zeros, how, over, status):
     assert _adamw_call(lib, zeros, 1, how, **over) == binding.STATUS[status]
 
 
+@pytest.mark.parametrize("eps", [1e-300, 1e-46, 1e-45, 1e-39, float(np.finfo(np.float32).tiny) * (1 - 2.0 ** -52), -1e-8,
+                                 float("nan"), float("inf"), 1e31])
+def test_adamw_refuses_an_eps_that_is_no_normal_fp32_number(lib, zeros, eps):
+    from paper_2602_01469_b200 import binding
+    assert _adamw_call(lib, zeros, 1, {"eps": eps}) == binding.STATUS["BAD_SHAPE"]
+
+
 def test_adamw_refuses_bad_lists(lib, zeros):
     from paper_2602_01469_b200 import binding
     import ctypes
