@@ -14,10 +14,10 @@
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, more than half of them integer ones for the random bits and the roundings: 91 M elements,
-// bf16, take 248 us, 57 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, 229, two or three
-// codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
-// a code whose number is near its border, and the largest number of a block near a power of two, are formed again in
-// fp64, and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
+// bf16, take 266 us, 53 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, some 20 us less, two or
+// three codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
+// a code whose number is near its border, the largest number of a block near a power of two, and in blocks of small roots
+// those whose v is below fp32's normal numbers, are formed again in fp64, and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
 // more instructions: 260 where this way took 254.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -270,6 +270,12 @@ __device__ __forceinline__ bool doubtful(uint32_t largest)
 {
     return largest >= 0x7f800000u || (largest > 0x0e000000u && (largest + 32u & 0x7fffffu) < 64u);
 }
+// From this root on, 2^-60, v is a normal number and the root right to a few units in the last place.  A v below 2^-126 may
+// be off by fp32's smallest number, 2^-149, and its root by 2^-76 then.
+constexpr float NORMAL_ROOT = 0x1p-60f;
+// That is 4 units in the last place of what is rounded to a code (2^-6 of the block's scale and more) where the largest root
+// of the block has these bits, 2^-41; where it is smaller, such roots are formed in fp64.
+constexpr uint32_t ROOM_FOR_SMALL_ROOTS = 0x2b000000u;
 
 __host__ __device__ inline Factors factors(const How &h, float lr, int64_t step)
 {
@@ -281,25 +287,27 @@ __host__ __device__ inline Factors factors(const How &h, float lr, int64_t step)
     return f;
 }
 
-// Approximate to about two units in the last place; numbers below 2^-126 count as 0.
+// Approximate to about two units in the last place, for numbers below 2^-126 too.  (They are v of gradients below 3e-18 on an
+// empty state.  With a root that took them for zero, 91 M elements with 8-bit states took 260 us instead of 266.)
 __device__ __forceinline__ float root_of(float v)
 {
     float r;
-    asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float quotient(float a, float b)
+// 1 / d for 2^-126 <= d <= 2^126, to a unit in the last place.
+__device__ __forceinline__ float reciprocal(float d)
 {
     float r;
-    asm("div.approx.ftz.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d));
     return r;
 }
 
 // p after a step, two elements; `decay` is -lr weight_decay.
 __device__ __forceinline__ F2 stepped(F2 p, F2 m, F2 root, const How &how, const Factors &f, float decay)
 {
-    const float2 d = unf2(fma_f2(root, f2(f.root_scale, f.root_scale), f2(how.eps, how.eps))), mv = unf2(m);
-    const F2 q = f2(quotient(mv.x, d.x), quotient(mv.y, d.y));
+    const float2 d = unf2(fma_f2(root, f2(f.root_scale, f.root_scale), f2(how.eps, how.eps))); // eps >= 2^-126
+    const F2 q = mul_f2(m, f2(reciprocal(d.x), reciprocal(d.y)));
     return fma_f2(q, f2(-f.step_size, -f.step_size), fma_f2(p, f2(decay, decay), p));
 }
 
@@ -338,16 +346,36 @@ __device__ __forceinline__ void exact_states(const How &how, float m0, float r0,
     root = __fsqrt_rn((float)__dadd_rn(__dmul_rn(how.beta2, (double)(r0 * r0)), __dmul_rn(__dmul_rn(1.0 - how.beta2, gd), gd)));
 }
 
+__device__ __forceinline__ float element(const void *p, int dtype, int64_t i)
+{
+    return dtype == PEAGLE_F32 ? static_cast<const float *>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]);
+}
+
 // What one element has in memory, and its new m and root.
 __device__ __forceinline__ void exact_element(const Tensor &t, const How &how, float grad_scale, int64_t i, float &m, float &root)
 {
     const float ms = t.m_scale[i / AW_BLOCK], vs = t.v_scale[i / AW_BLOCK];
-    const float g = t.grad_dtype == PEAGLE_F32 ? static_cast<const float *>(t.grad)[i]
-                                               : __bfloat162float(static_cast<const __nv_bfloat16 *>(t.grad)[i]);
+    const float g = element(t.grad, t.grad_dtype, i);
     float m0[8], r0[8];
     decode4(static_cast<const uint8_t *>(t.m)[i], m0, 0);
     decode4(static_cast<const uint8_t *>(t.v)[i], r0, 0);
     exact_states(how, m0[0] * ms, r0[0] * vs, g * grad_scale, m, root);
+}
+
+// The parameters of a thread's elements with small roots, from fp64's, where eps does not outweigh what these are off by.
+__device__ __forceinline__ void step_of_small_roots(const Tensor &t, const How &how, const Factors &f, float grad_scale, int64_t i,
+                                                    int left, const float (&r)[8], float (&p)[8])
+{
+#pragma unroll 1
+    for (int k = 0; k < left; ++k) {
+        float m, root;
+        exact_element(t, how, grad_scale, i + k, m, root);
+        const float p0 = t.master ? t.master[i + k] : element(t.param, t.param_dtype, i + k);
+        const float p1 = unf2(stepped(both(p0), both(m), both(root), how, f, -f.lr * t.weight_decay)).x;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            p[j] = j == k && r[j] < NORMAL_ROOT ? p1 : p[j];
+    }
 }
 
 // A thread's codes from fp64, where one of them was too near a border.  From memory, like the next.
@@ -391,7 +419,8 @@ __device__ __forceinline__ void exact_largest(const Tensor &t, const How &how, f
 
 // One thread's 8 elements of a tensor with states in 8 bits.  The whole warp, with a block of PEAGLE_ADAMW_BLOCK
 // elements; elements that are not there are zeros.
-template <bool VEC>
+// SMALL_EPS: see step_of_small_roots.
+template <bool VEC, bool SMALL_EPS>
 __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, const Factors &f, float grad_scale, uint32_t key,
                                             int64_t i, int left)
 {
@@ -427,13 +456,15 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
         m_min = fminf(fminf(m_min, fabsf(m[k])), fabsf(m[k + 1]));
         r_min = fminf(fminf(r_min, r[k]), r[k + 1]);
     }
+    if (SMALL_EPS && r_min < NORMAL_ROOT)
+        step_of_small_roots(t, how, f, grad_scale, i, left, r, p);
     if (t.master)
         store8<VEC>(t.master, PEAGLE_F32, i, left, p);
     store8<VEC>(t.param, t.param_dtype, i, left, p);
     uint32_t largest_m = __reduce_max_sync(~0u, __float_as_uint(m_max) & 0x7fffffffu);
     uint32_t largest_r = __reduce_max_sync(~0u, __float_as_uint(r_max) & 0x7fffffffu);
     bool finite = true;
-    if (doubtful(largest_m) || doubtful(largest_r)) {
+    if (doubtful(largest_m) || doubtful(largest_r) || largest_r - 1u < __float_as_uint(NORMAL_ROOT)) { // not zero
         finite = largest_m < 0x7f800000u && largest_r < 0x7f800000u;
         exact_largest(t, how, grad_scale, i, left, largest_m, largest_r);
     }
@@ -441,7 +472,7 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     const uint32_t first = key + (uint32_t)i * GOLDEN;
     const bool plain = finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f;
     const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
-    uint32_t nearness = ~0u;
+    uint32_t nearness = r_min < NORMAL_ROOT && largest_r - 1u < ROOM_FOR_SMALL_ROOTS ? 0u : ~0u;
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));
@@ -472,8 +503,8 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
 
 // KINDS: which states the list has, 1 in 32 bits, 2 in 8 bits, 3 both (with the registers of the larger).  8-bit states
 // alone are best with five blocks to an SM and 48 registers: with four they take 5 % longer, with six, which spill, 10 %.
-template <int N, int KINDS>
-__global__ void __launch_bounds__(AW_THREADS, KINDS == 2 ? 5 : 4) adamw_kernel(const __grid_constant__ Table<N> table)
+template <int N, int KINDS, bool SMALL_EPS>
+__global__ void __launch_bounds__(AW_THREADS, KINDS == 2 && !SMALL_EPS ? 5 : 4) adamw_kernel(const __grid_constant__ Table<N> table)
 {
     const How &how = table.how;
     Factors f = how.factors;
@@ -507,9 +538,9 @@ __global__ void __launch_bounds__(AW_THREADS, KINDS == 2 ? 5 : 4) adamw_kernel(c
         if (KINDS == 2 || (KINDS == 3 && t.m_scale)) {
             // a warp stays together, for its block's scales
             if (__all_sync(~0u, vec))
-                step8_codes<true>(t, how, f, grad_scale, key, i, left);
+                step8_codes<true, SMALL_EPS>(t, how, f, grad_scale, key, i, left);
             else
-                step8_codes<false>(t, how, f, grad_scale, key, i, left);
+                step8_codes<false, SMALL_EPS>(t, how, f, grad_scale, key, i, left);
         } else if (vec) {
             step8<true>(t, how, f, grad_scale, i, left);
         } else if (left) {
@@ -528,12 +559,14 @@ void launch_table(const How &how, const Tensor *t, int kinds, int n_sm, cudaStre
     // a block per chunk; where each has to form the factors, no more than fit the GPU
     const uint32_t most = how.lr_dev || how.step_dev ? 4u * n_sm : how.chunks;
     const uint32_t blocks = how.chunks < most ? how.chunks : most;
+    // the 2^-76 that a small root of 8-bit states may be off by, beside eps: below its rounding, or not
+    const bool small_eps = how.eps < 0x1p-52 / sqrt(1.0 - how.beta2);
     if (kinds == 1)
-        adamw_kernel<N, 1><<<blocks, AW_THREADS, 0, s>>>(table);
+        adamw_kernel<N, 1, false><<<blocks, AW_THREADS, 0, s>>>(table);
     else if (kinds == 2)
-        adamw_kernel<N, 2><<<blocks, AW_THREADS, 0, s>>>(table);
+        (small_eps ? adamw_kernel<N, 2, true> : adamw_kernel<N, 2, false>)<<<blocks, AW_THREADS, 0, s>>>(table);
     else
-        adamw_kernel<N, 3><<<blocks, AW_THREADS, 0, s>>>(table);
+        (small_eps ? adamw_kernel<N, 3, true> : adamw_kernel<N, 3, false>)<<<blocks, AW_THREADS, 0, s>>>(table);
 }
 
 } // namespace

@@ -197,6 +197,78 @@ def test_untouched_elements_stay_with_the_smallest_eps(ctx, bits):
     check(before, item, 0, 1, 2, how)
 
 
+def tiny_gradients(gen, n):
+    """From where v leaves fp32's normal numbers (1e-18) to where it is zero (1e-23), beside larger ones, zeros, and in
+    blocks of their own."""
+    tiny = torch.randn(n, generator=gen).sign() * 10 ** (-24 + 8 * torch.rand(n, generator=gen, dtype=torch.float64))
+    some = torch.rand(n, generator=gen) < 0.3
+    some[n // 2:] = True
+    # and blocks in between, some larger
+    rise = (10 ** (10 * torch.rand(n // 256 + 1, generator=gen))).repeat_interleave(256)[:n]
+    tiny[3 * n // 4:] *= rise[3 * n // 4:]
+    g = torch.where(some, tiny.float(), torch.randn(n, generator=gen) * 1e-3)
+    g[torch.rand(n, generator=gen) < 0.05] = 0
+    g[-600:] = 0
+    return g
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("empty", [True, False])
+def test_tiny_roots_are_kept_in_8_bits(ctx, dtype, empty):
+    """Every code is the defined one, and no root above zero is stored as zero, where v is no normal fp32 number; the
+    step divides by that root, whatever eps is."""
+    gen = torch.Generator().manual_seed(21)
+    n = 100_003
+    item = make(gen, n, dtype, dtype, 8, False, 0.1)
+    if empty:
+        for name in ("m", "v"):
+            item[name].view(torch.uint8).zero_()
+            item[name + "_scale"].zero_()
+    else:
+        item["v"].view(torch.uint8)[:] = torch.where(torch.rand(n, generator=gen) < 0.4, 0, item["v"].view(torch.uint8).cpu()).to(DEV)
+        item["v_scale"][::3] = 1e-22
+        item["m_scale"][::3] = 1e-23
+    item["grad"].copy_(tiny_gradients(gen, n))
+    how = dict(lr=3e-3, beta1=0.9, beta2=0.98, eps=1e-20)
+    tensors = binding.AdamWTensors([item])
+    code = lambda t: t.view(torch.uint8).cpu().numpy().ravel()
+    for step in (1, 2):
+        b = snapshot(item)
+        binding.peagle_adamw_step(ctx, tensors, step=step, seed=5, **how)
+        torch.cuda.synchronize()
+        _, root, mc, vc, _, _, ms, vs = oo.adamw_states8(f64(b["grad"]).ravel(), code(b["m"]), code(b["v"]), f64(b["m_scale"]),
+                                                         f64(b["v_scale"]), how["beta1"], how["beta2"], 5, step, 0)
+        assert np.array_equal(f64(item["m_scale"]), ms) and np.array_equal(f64(item["v_scale"]), vs)
+        values = oo.e4m3_values()
+        assert (values[code(item["v"])][root > 0] > 0).all()
+        for name, want in (("m", mc), ("v", vc)):
+            assert np.array_equal(values[code(item[name])], values[want], equal_nan=True), name
+        check(b, item, 0, step, 5, how)
+
+
+@pytest.mark.parametrize("eps", [2.0 ** -126, 1e-30, 1e-20, 1e-8])
+def test_tiny_roots_divide_the_step_in_32_bits(ctx, eps):
+    """The step from the m and v that are stored, which are fp32's, some of them no normal numbers."""
+    gen = torch.Generator().manual_seed(22)
+    n = 20_003
+    item = make(gen, n, F32, F32, 32, False, 0.0)
+    item["grad"].copy_(tiny_gradients(gen, n))
+    item["m"].zero_()
+    item["v"].zero_()
+    b = snapshot(item)
+    beta1, beta2, lr = 0.9, 0.98, 1e-3
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors([item]), step=1, lr=lr, beta1=beta1, beta2=beta2, eps=eps)
+    torch.cuda.synchronize()
+    m, v, g, p = f64(item["m"]), f64(item["v"]), f64(b["grad"]), f64(b["param"])
+    # fp32's smallest number is 2^-149; each of v's products and its sum is off by half of it at most
+    outside(m, (1 - beta1) * g, 5 * U * np.abs((1 - beta1) * g) + 2.0 ** -148)
+    outside(v, (1 - beta2) * g * g, 6 * U * (1 - beta2) * g * g + 2.0 ** -148)
+    assert (v[(np.abs(g) > 1e-21)] > 0).all()
+    update = lr * m / (1 - beta1) / (np.sqrt(v / (1 - beta2)) + eps)
+    want = p - update
+    outside(f64(item["param"]), want, 16 * U * np.abs(update) + 3 * U * (np.abs(p) + np.abs(update)) + U * np.abs(want))
+
+
 def test_states_that_begin_at_zero(ctx):
     gen = torch.Generator().manual_seed(7)
     item = make(gen, 700, F32, F32, 8, False, 0.0)
