@@ -14,10 +14,10 @@
 // the three mantissa bits that stay and cutting the rest off rounds up with the probability of the fraction.
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, more than half of them integer ones for the random bits and the roundings: 91 M elements,
-// bf16, take 266 us, 53 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, some 20 us less, two or
+// bf16, take 272 us, 52 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, some 20 us less, two or
 // three codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
 // a code whose number is near its border, the largest number of a block near a power of two, and in blocks of small roots
-// those whose v is below fp32's normal numbers, are formed again in fp64, and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
+// those whose v is below fp32's normal numbers, are formed again in fp64 (and so are blocks in which m cancels), and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
 // more instructions: 260 where this way took 254.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -277,6 +277,15 @@ constexpr float NORMAL_ROOT = 0x1p-60f;
 // of the block has these bits, 2^-41; where it is smaller, such roots are formed in fp64.
 constexpr uint32_t ROOM_FOR_SMALL_ROOTS = 0x2b000000u;
 
+// Whether m's two terms have cancelled in a whole block: `old` is beta1 times its old scale, so its terms were up to 256 times
+// that.  In fp32 they leave up to 2^-30 of the scale (see below), a few units in the last place of what is rounded to a code
+// unless the largest m is a fourth of what it was or less; then the block is formed in fp64.  (Not where the old scale is
+// the least there is, and means nothing.)
+__device__ __forceinline__ bool all_cancelled(uint32_t largest, float old)
+{
+    return __uint_as_float(largest) < 32.f * old && old > 0x1p-107f;
+}
+
 __host__ __device__ inline Factors factors(const How &h, float lr, int64_t step)
 {
     Factors f;
@@ -441,8 +450,8 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const F2 gg = mul_f2(f2(g[k], g[k + 1]), f2(grad_scale, grad_scale));
-        // b1_top's product with a code is exact and the rest is 2^-16 of it, so m is right to a few units in the last
-        // place where up to 2^19 of its terms cancels; what is smaller is far below a code's spacing
+        // b1_top's product with a code is exact and the rest is 2^-16 of it, so m is off by 2^-38 of its terms and a few
+        // units in the last place of its own: far below a code's spacing, unless the terms cancel in the whole block
         const F2 code = f2(m[k], m[k + 1]), rest = fma_f2(c1_rest, gg, mul_f2(b1_rest, code));
         const F2 m2 = add_f2(fma_f2(c1, gg, mul_f2(b1, code)), rest);
         const F2 r0 = mul_f2(f2(r[k], r[k + 1]), vs2);
@@ -464,15 +473,17 @@ __device__ __forceinline__ void step8_codes(const Tensor &t, const How &how, con
     uint32_t largest_m = __reduce_max_sync(~0u, __float_as_uint(m_max) & 0x7fffffffu);
     uint32_t largest_r = __reduce_max_sync(~0u, __float_as_uint(r_max) & 0x7fffffffu);
     bool finite = true;
-    if (doubtful(largest_m) || doubtful(largest_r) || largest_r - 1u < __float_as_uint(NORMAL_ROOT)) { // not zero
+    bool cancelled = all_cancelled(largest_m, b1s);
+    if (doubtful(largest_m) || doubtful(largest_r) || cancelled || largest_r - 1u < __float_as_uint(NORMAL_ROOT)) { // not zero
         finite = largest_m < 0x7f800000u && largest_r < 0x7f800000u;
         exact_largest(t, how, grad_scale, i, left, largest_m, largest_r);
+        cancelled = all_cancelled(largest_m, b1s);
     }
     const float2 sm = scale_of(__uint_as_float(largest_m)), sv = scale_of(__uint_as_float(largest_r));
     const uint32_t first = key + (uint32_t)i * GOLDEN;
     const bool plain = finite && m_min * sm.y >= 0.015625f && r_min * sv.y >= 0.015625f;
     const F2 sm2 = f2(sm.y, sm.y), sv2 = f2(sv.y, sv.y);
-    uint32_t nearness = r_min < NORMAL_ROOT && largest_r - 1u < ROOM_FOR_SMALL_ROOTS ? 0u : ~0u;
+    uint32_t nearness = cancelled || (r_min < NORMAL_ROOT && largest_r - 1u < ROOM_FOR_SMALL_ROOTS) ? 0u : ~0u;
 #pragma unroll
     for (int k = 0; k < 8; k += 2) {
         const float2 a = unf2(mul_f2(f2(m[k], m[k + 1]), sm2)), b = unf2(mul_f2(f2(r[k], r[k + 1]), sv2));

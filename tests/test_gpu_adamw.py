@@ -197,6 +197,36 @@ def test_untouched_elements_stay_with_the_smallest_eps(ctx, bits):
     check(before, item, 0, 1, 2, how)
 
 
+@pytest.mark.parametrize("beta1", [0.9, 0.95, 0.5, 0.0])
+def test_blocks_whose_average_cancels(ctx, beta1):
+    """m = beta1 m + (1 - beta1) g of nearly nothing in all elements of a block: codes and scales are those of fp64."""
+    rng = np.random.default_rng(31)
+    values = oo.e4m3_values()
+    items = []
+    for k in range(400):
+        n = 1 if k < 300 else 1 + k % 256
+        # one code for a block, mostly: what cancels in one element cancels in all of them
+        c = rng.integers(0x50, 0x78, n if k % 3 == 0 else 1).astype(np.uint8) | (128 * rng.integers(0, 2, 1)).astype(np.uint8)
+        c = np.broadcast_to(c, n).copy()
+        scale = 2.0 ** rng.integers(-20, 5)
+        g = -(beta1 / (1 - beta1)) * values[c] * scale
+        g = g * (1 + (0.0, 2.0 ** -22, -2.0 ** -18, 2.0 ** -12, 2.0 ** -6)[k % 5]) if beta1 else values[c] * scale * 2.0 ** -(k % 30)
+        item = {"param": torch.zeros(n, device=DEV), "grad": torch.tensor(g, dtype=F32, device=DEV), "weight_decay": 0.0,
+                "master": None, "m": torch.tensor(c, device=DEV).view(F8), "m_scale": torch.full((1,), scale, device=DEV),
+                "v": torch.tensor(c & 127, device=DEV).view(F8), "v_scale": torch.full((1,), scale, device=DEV)}
+        items.append(item)
+    before = [snapshot(i) for i in items]
+    how = dict(lr=1e-3, beta1=beta1, beta2=0.98, eps=1e-8)
+    binding.peagle_adamw_step(ctx, binding.AdamWTensors(items), step=3, seed=6, **how)
+    torch.cuda.synchronize()
+    code = lambda t: t.view(torch.uint8).cpu().numpy().ravel()
+    for k, (b, a) in enumerate(zip(before, items)):
+        _, _, mc, vc, _, _, ms, vs = oo.adamw_states8(f64(b["grad"]), code(b["m"]), code(b["v"]), f64(b["m_scale"]),
+                                                      f64(b["v_scale"]), beta1, how["beta2"], 6, 3, k)
+        assert np.array_equal(f64(a["m_scale"]), ms) and np.array_equal(f64(a["v_scale"]), vs), (k, f64(a["m_scale"]), ms)
+        assert np.array_equal(values[code(a["m"])], values[mc]) and np.array_equal(values[code(a["v"])], values[vc]), k
+
+
 def tiny_gradients(gen, n):
     """From where v leaves fp32's normal numbers (1e-18) to where it is zero (1e-23), beside larger ones, zeros, and in
     blocks of their own."""
