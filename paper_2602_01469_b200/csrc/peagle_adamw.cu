@@ -264,11 +264,11 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-// Whether a block whose largest magnitude has these bits is done over: not finite, or so near a power of two that
-// fp32's roundings may have carried it across.
+// Whether a block whose largest magnitude has these bits is done over: not finite, or so near a power of two, from 2^-99 on,
+// that fp32's roundings may have carried it across.
 __device__ __forceinline__ bool doubtful(uint32_t largest)
 {
-    return largest >= 0x7f800000u || (largest > 0x0e000000u && (largest + 32u & 0x7fffffu) < 64u);
+    return largest >= 0x7f800000u || (largest > 0x0dffff00u && (largest + 32u & 0x7fffffu) < 64u);
 }
 // From this root on, 2^-60, v is a normal number and the root right to a few units in the last place.  A v below 2^-126 may
 // be off by fp32's smallest number, 2^-149, and its root by 2^-76 then.

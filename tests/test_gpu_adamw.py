@@ -227,6 +227,21 @@ def test_blocks_whose_average_cancels(ctx, beta1):
         assert np.array_equal(values[code(a["m"])], values[mc]) and np.array_equal(values[code(a["v"])], values[vc]), k
 
 
+@pytest.mark.parametrize("power", [-100, -99, -98, -60, 0])
+def test_scales_next_to_a_power_of_two(ctx, power):
+    """Blocks whose m is the power of two, or a few units in the last place to either side; 2^-99 is the first that moves
+    the scale."""
+    for beta1 in (0.9, 0.85, 0.8, 0.7, 0.6):
+        at = int(np.float32(2.0 ** power / (1 - beta1)).view(np.int32))
+        g = np.arange(at - 20, at + 20, dtype=np.int32).view(np.float32)
+        zero = lambda dtype: torch.zeros(1, dtype=torch.uint8, device=DEV).view(F8) if dtype == F8 else torch.zeros(1, device=DEV)
+        items = [{"param": zero(F32), "grad": torch.tensor([x], device=DEV), "m": zero(F8), "v": zero(F8), "m_scale": zero(F32),
+                  "v_scale": zero(F32)} for x in g]
+        binding.peagle_adamw_step(ctx, binding.AdamWTensors(items), step=1, lr=1e-3, beta1=beta1, beta2=0.98, eps=1e-8)
+        want = oo.block_scale(((1 - beta1) * g.astype(np.float64)).astype(np.float32).astype(np.float64), 1)
+        assert np.array_equal(torch.cat([i["m_scale"] for i in items]).double().cpu().numpy(), want), beta1
+
+
 def tiny_gradients(gen, n):
     """From where v leaves fp32's normal numbers (1e-18) to where it is zero (1e-23), beside larger ones, zeros, and in
     blocks of their own."""
