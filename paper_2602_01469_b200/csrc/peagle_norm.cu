@@ -262,6 +262,11 @@ constexpr int fwd_blocks(bool layer, int words, int tpr, int threads)
     const int want = words > 8 || tpr < 32 ? 512 : tpr == 512 ? 1024 : 768;
     return want < threads ? 1 : want / threads;
 }
+// Whether the mean takes the sum of what is left, x - mu, as its correction: its own sum has lost more digits than the
+// differences then.  Those are rounded alike within a binade, which adds up: 2,880 bf16 numbers of spread 2.2 have a mean off
+// by 2e-9 as summed and by 4e-8 corrected around 0, both 6e-8 around 1, 3e-5 and 2e-5 around 1,000.
+__device__ __forceinline__ bool off_centre(float mu, float var) { return !(16.f * mu * mu < var); }
+
 template <class T, bool VEC, int TPR, int E>
 __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __grid_constant__ NormArgs a)
 {
@@ -325,8 +330,8 @@ __global__ void __launch_bounds__(block_threads(TPR)) norm_fwd_kernel(const __gr
             const float2 s2 = unf2(s), q2 = unf2(q);
             const float2 both = group_sum2<TPR>(f2(s2.x + s2.y, q2.x + q2.y), red2, turn);
             const float left = both.x * per_col; // the rounding of mu is taken out of both
-            mu += left;
             var = both.y * per_col - left * left;
+            mu += off_centre(mu, var) ? left : 0.f;
         } else {
             F2 q = f2(0.f, 0.f);
 #pragma unroll
@@ -608,8 +613,8 @@ __global__ void __launch_bounds__(ROW_THREADS) norm_fwd_rows(const NormArgs a)
         }
         const float2 t = block_sum(s, q);
         const float left = a.kind == PEAGLE_NORM_LAYER ? t.x / a.cols : 0.f;
-        mu += left;
         const float var = t.y / a.cols - left * left;
+        mu += off_centre(mu, var) ? left : 0.f;
         const float rstd = rsqrtf((var < 0.f ? 0.f : var) + a.eps);
         for (int c = threadIdx.x; c < a.cols; c += ROW_THREADS)
             store1(y + c, fmaf((load1(x + c) - mu) * rstd, load_w(a.weight, a.w_dtype, c, 1.f),

@@ -200,6 +200,28 @@ def test_rows_of_very_large_and_very_small_numbers(ctx, kind, dtype, cols):
     check_bwd(kind, x, w, m, rstd, dy, dx, dw, zero, db, zero)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("cols", [1001, 2880, 5120, 18000])
+def test_the_mean_of_centred_and_shifted_rows(ctx, dtype, cols):
+    """Rows around 0, spread s: an addition is off by U / sqrt(3) of its result in the mean square.  A thread's chains, in
+    two halves, add up to 16 elements or cols / 256, a warp joins 32 and a block its warps: with partial sums that grow
+    like the root of their number, an error of the mean of U s sqrt((11 / cols + 1 / 512) / 3), of which three times are
+    allowed over 512 rows.  Around 1 and 1,000 the sum of the differences corrects the mean: its own rounding, U |mean|,
+    and those of the differences, at most U of each, 4 U s with what their sum loses."""
+    gen = torch.Generator().manual_seed(cols + 1)
+    rows, s = 512, 2.2
+    for middle in (0.0, 1.0, 1000.0):
+        x = (middle + s * torch.randn(rows, cols, generator=gen)).to(dtype).to(DEV)
+        y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=DEV), torch.empty(rows, device=DEV)
+        binding.peagle_norm_fwd(ctx, 0, x, None, None, 1e-5, y, mean, rstd)
+        check_fwd("layer", x, None, None, 1e-5, y, mean, rstd)
+        off = f64(mean) - f64(x).mean(1)
+        if middle == 0.0:
+            assert np.sqrt((off ** 2).mean()) <= 3 * U32 * s * np.sqrt((11 / cols + 1 / 512) / 3)
+        else:
+            assert np.abs(off).max() <= U32 * (1.01 * middle + 4 * s)
+
+
 def test_nan_and_infinity_stay_in_their_rows(ctx):
     gen = torch.Generator().manual_seed(6)
     for cols in (128, 2880, 1001):
