@@ -290,15 +290,17 @@ class AdamWTensors:
         self.set_grads([i["grad"] for i in self.items])
 
     def set_grads(self, grads):
-        """Other gradients for the steps to come, in the order of the tensors."""
+        """Other gradients for the steps to come, in the order of the tensors.  All of them are taken, or none."""
         grads = list(grads)
         if len(grads) != len(self.items):
             _refuse()
-        for c, i, g in zip(self.c, self.items, grads):
+        fresh = []
+        for c, g in zip(self.c, grads):
             if g.get_device() != self.device or g.numel() != c.count or not g.is_contiguous():
                 _refuse()
-            c.grad, c.grad_dtype = g.data_ptr(), _dtype(g)
-            i["grad"] = g
+            fresh.append((g.data_ptr(), _dtype(g)))
+        for c, i, g, (at, code) in zip(self.c, self.items, grads, fresh):
+            c.grad, c.grad_dtype, i["grad"] = at, code, g
 
 
 class Context:

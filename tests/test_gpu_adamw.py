@@ -423,3 +423,26 @@ def test_set_grads_and_refusals(ctx):
     refused("BAD_SHAPE", tensors.set_grads, [])
     refused("BAD_SHAPE", binding.peagle_adamw_step, ctx, tensors, 1e-3, 0.9, 0.99, 1e-8, step=0)
     refused("BAD_SHAPE", binding.peagle_adamw_step, ctx, tensors, 1e-3, 0.9, 0.99, 1e-8, step_dev=torch.ones(1, device=DEV))
+
+
+def test_refused_gradients_leave_the_old_ones(ctx):
+    """A list that is refused half way changes nothing: the next step takes all gradients from the list before."""
+    gen = torch.Generator().manual_seed(14)
+    items = [make(gen, n, BF16, BF16, 32, False, 0.0) for n in (300, 40, 7)]
+    tensors = binding.AdamWTensors(items)
+    old = [i["grad"] for i in tensors.items]
+    pointers = [(c.grad, c.grad_dtype) for c in tensors.c]
+    fresh = [torch.randn(n, generator=gen).to(DEV) for n in (300, 40, 7)]
+    for bad in (fresh[2][:6], fresh[2].half(), fresh[2].cpu()):
+        with pytest.raises(binding.PeagleError) as e:
+            tensors.set_grads([fresh[0], fresh[1], bad])
+        assert e.value.status == binding.STATUS["BAD_SHAPE"]
+        assert [(c.grad, c.grad_dtype) for c in tensors.c] == pointers
+        assert all(i["grad"] is g for i, g in zip(tensors.items, old))
+    tensors.set_grads(fresh)
+    assert [c.grad for c in tensors.c] == [g.data_ptr() for g in fresh]
+    before = [snapshot(i) for i in tensors.items]
+    binding.peagle_adamw_step(ctx, tensors, step=1, **HOW)
+    torch.cuda.synchronize()
+    for k, (b, a) in enumerate(zip(before, tensors.items)):
+        check(b, a, k, 1, 0)
