@@ -320,3 +320,32 @@ def test_binding_refuses_host_tensors(lib):
         with pytest.raises(b.PeagleError) as e:
             call()
         assert e.value.status == b.STATUS["BAD_SHAPE"]
+
+
+@pytest.mark.parametrize("rows,cols", [(1 << 31, 1), (1 << 32, 1), ((1 << 32) + 3, 1), (1, (1 << 32) + 3), (2, 1 << 31)])
+def test_binding_refuses_sizes_past_int32(lib, zeros, rows, cols):
+    """A size whose lower 32 bits are an ordinary size, or none: it must not be taken for that one.  (On tensors without
+    memory; a call that came to the library would find NULL, or no rows to do.)"""
+    import ctypes
+    from paper_2602_01469_b200 import binding as b
+    b._know_torch()
+
+    class ctx:
+        h, device = ctypes.addressof(zeros), -1
+
+    def meta(*shape, dtype=torch.bfloat16):
+        return torch.empty(*shape, dtype=dtype, device="meta")
+
+    x, f, i = meta(rows, cols), meta(rows, dtype=torch.float32), meta(rows, dtype=torch.int32)
+    calls = [
+        lambda: b.peagle_norm_fwd(ctx, 1, x, None, None, 1e-5, x, None, f, stream=0),
+        lambda: b.peagle_norm_bwd(ctx, 1, x, None, None, f, x, x, stream=0),
+        lambda: b.peagle_token_logprobs_fwd(ctx, x, i, 1.0, f, stream=0),
+        lambda: b.peagle_token_logprobs_bwd(ctx, x, i, 1.0, f, None, f, None, x, stream=0),
+        lambda: b.peagle_token_logprobs_fwd(ctx, meta(1, 4), i[:1], 1.0, f[:1], top_logprobs=meta(1, max(rows, cols), dtype=torch.float32),
+                                            top_ids=meta(1, max(rows, cols), dtype=torch.int32), stream=0),
+    ]
+    for call in calls:
+        with pytest.raises(b.PeagleError) as e:
+            call()
+        assert e.value.status == b.STATUS["TOO_LARGE"]
