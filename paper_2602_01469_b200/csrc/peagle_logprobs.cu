@@ -150,8 +150,7 @@ __device__ __forceinline__ void write_row(const LogprobArgs &a, int r, const Row
         lp = 0.f;
     else if (token < 0 || token >= a.vocab) {
         lp = nan_f32();
-        if (a.logprob)
-            atomicCAS(a.status, 0, PEAGLE_ERR_BAD_META);
+        atomicCAS(a.status, 0, PEAGLE_ERR_BAD_META);
     }
     if (a.logprob)
         a.logprob[r] = lp;

@@ -288,6 +288,20 @@ def test_tokens_outside_the_vocabulary_are_reported(ctx):
     assert binding.peagle_poll_status(ctx) == binding.STATUS["BAD_META"]
 
 
+def test_tokens_outside_are_reported_whatever_is_asked_for(ctx):
+    x = torch.randn(4, 100, device=DEV)
+    lse, top, ids = torch.empty(4, device=DEV), torch.empty(4, 3, device=DEV), torch.empty(4, 3, dtype=torch.int32, device=DEV)
+    good = torch.tensor([1, 99, -1, 5], dtype=torch.int32, device=DEV)
+    for bad in (100, -2, -2 ** 31):
+        tokens = torch.tensor([1, bad, -1, 5], dtype=torch.int32, device=DEV)
+        for outputs in ((None, lse), (None, None, lse), (None, None, None, top, ids)):
+            binding.peagle_token_logprobs_fwd(ctx, x, tokens, 1.0, *outputs)
+            assert binding.peagle_poll_status(ctx) == binding.STATUS["BAD_META"]
+            binding.peagle_token_logprobs_fwd(ctx, x, good, 1.0, *outputs)
+            binding.peagle_token_logprobs_fwd(ctx, x, None, 1.0, *outputs)
+            assert binding.peagle_poll_status(ctx) == 0
+
+
 @pytest.mark.parametrize("scale", [1e-20, 1e-3, 50.0, 1e20])
 def test_scales_far_from_one(ctx, scale):
     """Nearly uniform rows, rows with one token left, and logits that the scale takes past fp32's range."""
