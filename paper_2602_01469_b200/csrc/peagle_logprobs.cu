@@ -778,12 +778,12 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
 constexpr int FWD_SMEM = STAGES * FWD_PIECES * LP_THREADS * 16;
 
 // Whether the GPU places clusters of 16 blocks of a kernel, more than every GPU has to.  Asked once per kernel (all
-// devices here are alike).
-template <class Kernel>
-bool takes_16(Kernel kernel)
+// devices here are alike), which is the template's argument: the instances share a type, not registers and shared memory.
+template <auto KERNEL>
+bool takes_16()
 {
     static std::atomic<int> known; // 0 not asked, 1 no, 2 yes
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
+    if (cudaFuncSetAttribute(KERNEL, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) {
         cudaGetLastError();
         return false;
     }
@@ -799,7 +799,7 @@ bool takes_16(Kernel kernel)
         cfg.attrs = at;
         cfg.numAttrs = 1;
         int n = 0;
-        const bool yes = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess && n > 0;
+        const bool yes = cudaOccupancyMaxActiveClusters(&n, KERNEL, &cfg) == cudaSuccess && n > 0;
         if (!yes)
             cudaGetLastError();
         known.store(yes ? 2 : 1, std::memory_order_relaxed);
@@ -810,13 +810,13 @@ bool takes_16(Kernel kernel)
 template <class T, bool ENTROPY, bool TOP>
 void forward(const LogprobArgs &a, int n_sm, cudaStream_t s)
 {
-    const auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
+    constexpr auto kernel = logprobs_fwd_kernel<T, ENTROPY, TOP>;
     // few rows are cut as long as the GPU has places left
     int parts = 1;
     while (parts < 8 && (int64_t)a.rows * parts * 2 <= 8 * n_sm && a.vocab / (parts * 2) >= LEAST_PART)
         parts *= 2;
     // clusters of 16 are harder to place: 16 rows of 128,000 take 20.7 us with them and 14.4 without, one 13.3 and 13.4
-    if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED && takes_16(kernel))
+    if (parts == 8 && a.rows <= 4 && a.vocab / 16 >= LEAST_PART && 16 * a.top_k <= COUNTED && takes_16<kernel>())
         parts = 16;
     const int part_len = ((a.vocab + parts - 1) / parts + 7) / 8 * 8;
     cudaLaunchConfig_t cfg = {};

@@ -208,6 +208,31 @@ def test_rows_where_it_can_go_wrong(ctx, dtype, vocab, k, repeat):
     check_backward(ctx, x, tokens, 1.0, got[1], None, g, None)
 
 
+def forward_without_entropy(ctx, x, tokens, scale, k):
+    rows = x.shape[0]
+    lp, lse = torch.full((rows,), float("nan"), device=DEV), torch.full((rows,), float("nan"), device=DEV)
+    top = torch.full((rows, k), float("nan"), device=DEV) if k else None
+    ids = torch.full((rows, k), -7, dtype=torch.int32, device=DEV) if k else None
+    binding.peagle_token_logprobs_fwd(ctx, x, tokens, scale, lp, lse, None, top, ids)
+    torch.cuda.synchronize()
+    return lp, lse, top, ids
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("k", [0, 20, 64])
+@pytest.mark.parametrize("rows", [1, 4, 5])
+def test_few_long_rows_in_every_form(ctx, dtype, k, rows):
+    """Clusters of 16 blocks, or of 8: with entropy and without, with alternatives and without."""
+    vocab = 70001
+    gen = torch.Generator().manual_seed(rows)
+    x = put((3 * torch.randn(rows, vocab, generator=gen)).to(dtype))
+    tokens = torch.randint(-1, vocab, (rows,), generator=gen).to(torch.int32).to(DEV)
+    got = forward(ctx, x, tokens, 1.0, k)
+    check_forward(x, tokens, 1.0, k, got)
+    lp, lse, top, ids = forward_without_entropy(ctx, x, tokens, 1.0, k)
+    check_forward(x, tokens, 1.0, k, (lp, lse, got[2], top, ids))
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("repeat", [1, 130]) # rows cut into parts, and whole ones
 def test_rows_that_overflow_the_list_late(ctx, dtype, repeat):
