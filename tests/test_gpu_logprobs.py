@@ -219,6 +219,20 @@ def forward_without_entropy(ctx, x, tokens, scale, k):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("k", [0, 20])
+@pytest.mark.parametrize("vocab,repeat", [(1003, 1), (20011, 1), (5000, 14)])
+def test_rows_where_it_can_go_wrong_without_entropy(ctx, dtype, k, vocab, repeat):
+    x = special_rows(vocab, dtype).repeat(repeat, 1)
+    gen = torch.Generator().manual_seed(k + 1)
+    tokens = torch.randint(-1, vocab, (x.shape[0],), generator=gen).to(torch.int32).to(DEV)
+    x = put(x, 0, 0)
+    lp, lse, top, ids = forward_without_entropy(ctx, x, tokens, 1.0, k)
+    # the entropy's place is filled with the definition's: it is not asked for
+    H = oo.token_logprobs(x.double().cpu().numpy(), tokens.cpu().numpy(), 1.0, k)[2]
+    check_forward(x, tokens, 1.0, k, (lp, lse, torch.tensor(H, device=DEV), top, ids))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("k", [0, 20, 64])
 @pytest.mark.parametrize("rows", [1, 4, 5])
 def test_few_long_rows_in_every_form(ctx, dtype, k, rows):
@@ -388,6 +402,28 @@ def test_rows_past_two_to_the_31_elements(ctx):
     want = oo.token_logprobs_bwd(first.double().cpu().numpy(), tokens[at].cpu().numpy(), 1.0, lse[at].cpu().numpy(), None,
                                  np.ones(5), None)
     assert np.allclose(x[at].double().cpu().numpy(), want, rtol=2.0 ** -7, atol=1e-6)
+    del buf, x
+
+
+def test_entropies_past_two_to_the_31_elements(ctx):
+    rows, ld = 2200, 1000003
+    buf = torch.zeros(rows * ld, dtype=BF16, device=DEV)
+    x = buf.view(rows, ld)[:, :300]
+    x.copy_(torch.randn(rows, 300, device=DEV))
+    tokens = torch.randint(300, (rows,), device=DEV).to(torch.int32)
+    lp, lse, H, h = (torch.empty(rows, device=DEV) for _ in range(4))
+    binding.peagle_token_logprobs_fwd(ctx, x, tokens, 1.0, lp, lse, H)
+    binding.peagle_token_logprobs_fwd(ctx, x, tokens, 1.0, None, None, h)
+    assert torch.equal(H, h)
+    at = [0, 1, 2147, 2148, 2199]
+    check_forward(x[at].clone(), tokens[at], 1.0, 0, (lp[at], lse[at], H[at], None, None))
+    g, first = torch.randn(rows, device=DEV), x[at].clone()
+    binding.peagle_token_logprobs_bwd(ctx, x, tokens, 1.0, lse, H, g, lp, x)     # in place
+    torch.cuda.synchronize()
+    want = torch.empty_like(first)
+    binding.peagle_token_logprobs_bwd(ctx, first, tokens[at], 1.0, lse[at], H[at], g[at], lp[at], want)
+    assert torch.equal(x[at], want)
+    check_backward(ctx, first, tokens[at], 1.0, lse[at], H[at], g[at], lp[at])
     del buf, x
 
 
