@@ -648,16 +648,16 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
     if (fabsf(s.m) < INF && fabsf(s.m * l) >= REFERENCE_LARGE) {
         // a row of numbers far from zero, masked throughout for one: again, with x - m in the place of x
         const float m = s.m;
-        float S = 0.f, E = 0.f;
+        double S = 0.0, E = 0.0; // long sums of single entries
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
             const float t = (to_f32(row[j]) - m) * l, p = fast_exp2(t);
             S += p;
-            E = fmaf(p, fmaxf(t, T_FLOOR), E);
+            E += p * fmaxf(t, T_FLOOR);
         }
-        S = block_join(S, [](float p, float q) { return p + q; });
-        E = block_join(E, [](float p, float q) { return p + q; });
+        S = block_join(S, [](double p, double q) { return p + q; });
+        E = block_join(E, [](double p, double q) { return p + q; });
         if (threadIdx.x == 0) {
-            stats = row_stats({m, S, E}, 0.f, a.scale);
+            stats = row_stats({m, (float)S, (float)E}, 0.f, a.scale);
             write_row(a, r, stats, x_token, token);
         }
         __syncthreads();
@@ -700,13 +700,14 @@ __global__ void __launch_bounds__(LP_THREADS) logprobs_bwd_kernel(const __grid_c
         // from the row itself: one block, so that dlogits may be logits
         if (part != 0)
             return;
-        float m = -INF, S = 0.f;
+        float m = -INF;
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
             m = fmaxf(m, to_f32(row[j]));
         m = block_join(m, [](float p, float q) { return fmaxf(p, q); });
+        double S = 0.0; // a long sum of single entries
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS)
             S += fast_exp2((to_f32(row[j]) - m) * a.scale * LOG2E);
-        const float logS = logf(block_join(S, [](float p, float q) { return p + q; }));
+        const float logS = logf((float)block_join(S, [](double p, double q) { return p + q; }));
         for (int j = threadIdx.x; j < a.vocab; j += LP_THREADS) {
             const float t = (to_f32(row[j]) - m) * a.scale - logS, p = fast_exp2(t * LOG2E);
             from_f32(out + j, j == token ? of_token(t) : a.scale * p * (-g - h * (fmaxf(t, T_FLOOR) + H)));

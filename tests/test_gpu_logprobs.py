@@ -303,6 +303,32 @@ def test_a_peaked_row_keeps_its_digits(ctx):
     assert float(d[0, 77]) == pytest.approx(-math.expm1(40.0 - float(got[1][0])), rel=1e-5, abs=1e-12)
 
 
+@pytest.mark.parametrize("step", [1.203125, 0.703125, 3.109375])
+def test_long_rows_far_from_zero_keep_their_sums(ctx, step):
+    """Rows of 2^21 entries around 100,000, which are summed again one by one: the sum of as many like terms stays as good
+    as its terms.  A term is off by U (4 |t| + 8), |t| = step at most; logS, about 14, and what is formed with it are
+    rounded: 64 U of logprob, and of a gradient, in which t = scale x - logS becomes relative, 128 U.  The entropy has
+    log S and E / S, each to 64 U."""
+    vocab = 1 << 21
+    row = torch.full((vocab,), 100000.0)
+    row[1::2] -= step
+    row[3::8] -= step
+    x = torch.stack((row, row.flip(0), row)).to(DEV)
+    x[2] *= -1
+    tokens = torch.tensor([0, 1, 3], dtype=torch.int32, device=DEV)
+    lp, lse, H, top, ids = forward(ctx, x, tokens, 1.0, 2)
+    want, _, wH, wtop, wids = oo.token_logprobs(x.double().cpu().numpy(), tokens.cpu().numpy(), 1.0, 2)
+    assert np.array_equal(ids.cpu().numpy(), wids)
+    near(lp, want, 64 * U * np.ones(3))
+    near(top, wtop, 64 * U * np.ones((3, 2)))
+    near(H, wH, 2 * 64 * U * np.ones(3))
+    g = torch.tensor([1.0, -2.0, 0.5], device=DEV)
+    d = torch.empty_like(x)
+    binding.peagle_token_logprobs_bwd(ctx, x, tokens, 1.0, lse, None, g, None, d)
+    w = oo.token_logprobs_bwd(x.double().cpu().numpy(), tokens.cpu().numpy(), 1.0, lse.double().cpu().numpy(), None, g.cpu().numpy(), None)
+    near(d, w, 128 * U * np.abs(w))
+
+
 def test_zero_gradients_skip_the_row(ctx):
     x = torch.full((3, 3001), float("nan"), dtype=BF16, device=DEV)
     x[1] = 1.0
