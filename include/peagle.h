@@ -322,7 +322,8 @@ typedef enum peagle_dtype { PEAGLE_F32 = 0, PEAGLE_BF16 = 1 } peagle_dtype;
  * X, Y are dev [rows][cols] of x_dtype; weight, bias dev [cols] of w_dtype, each may be NULL (1 and 0).
  * mean, rstd are dev fp32 [rows], what the backward needs; each may be NULL (mean is not written by
  * PEAGLE_NORM_RMS).  eps > 0, cols <= 2^30 (up to 16,384 a row is read once).  In place: Y may be X with
- * the same leading dimension.  A NaN or infinity stays in its row.  Asynchronous.
+ * the same leading dimension.  A NaN or infinity stays in its row.  Sums are fp32: a row whose sum of squares
+ * passes 3.4e38 (numbers of 1e17 and more) counts as one of infinite variance, rstd 0.  Asynchronous.
  */
 typedef enum peagle_norm { PEAGLE_NORM_LAYER = 0, PEAGLE_NORM_RMS = 1 } peagle_norm;
 int peagle_norm_fwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dtype, int32_t rows,
@@ -358,7 +359,8 @@ int peagle_norm_bwd(peagle_ctx *ctx, int32_t kind, int32_t x_dtype, int32_t w_dt
  *     ids 0, 1, .. with log probability -inf;
  *   - a row with a NaN or +inf has NaN in all its fp32 outputs (0 for the logprob of token -1), top ids -1;
  *   - a token outside [-1, vocab) gets logprob NaN and sets PEAGLE_ERR_BAD_META in the status word.
- * Nothing depends on the order in which blocks finish.  Asynchronous.
+ * Nothing depends on the order in which blocks finish.  (A row whose maximum times scale is 45,000 or more in
+ * magnitude is read once more, for sums of exact differences, by one block.)  Asynchronous.
  */
 #define PEAGLE_MAX_TOP_K 64
 int peagle_token_logprobs_fwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int32_t vocab,
@@ -397,13 +399,16 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
  * the probability of the fraction, because to the nearest an average with beta2 near 1 would never move: its steps
  * are smaller than half a code.  (A root above zero is never stored as zero, it divides the next step.)  The random
  * bits are a hash of (seed, step, place of the tensor in the list, element), so a step repeats bit for bit.  The new
- * m and v are as from fp64, rounded to fp32 once, and the root is fp32's, before codes are taken.  An element whose new state is not finite is stored as NaN and does not
- * count for its block's scale.  All zero codes and any finite scales are the states to begin with.
+ * m and v are as from fp64, rounded to fp32 once, and the root is fp32's, before codes are taken.  An element whose
+ * new state is not finite is stored as NaN and does not count for its block's scale.  All zero codes and any finite
+ * scales are the states to begin with.
+ *   Either way v is an fp32 number: with beta2 = 0.999 and an empty state it is zero for gradients below 1e-21, where
+ * the step divides by eps alone, and infinite for gradients above 5e20.
  * lr_dev, step_dev, grad_scale_dev (dev, each may be NULL) replace lr, step and the factor 1, so that a captured
  * graph can be replayed with others.  lr >= 0, 0 <= beta < 1, weight_decay >= 0, step >= 1 (not checked on the device);
  * eps >= 2^-126, fp32's smallest normal number: the step is taken in fp32, where a smaller one could count as zero and
- * an element with m = v = 0 become 0 / 0.  Tensors must not share memory.  `tensors` is a host array, read before the
- * call returns; a launch takes PEAGLE_ADAMW_TENSORS of them.  Asynchronous; nothing is allocated.
+ * an element with m = v = 0 become 0 / 0.  Tensors must not share memory, nor with gradients.  `tensors` is a host
+ * array, read before the call returns; a launch takes PEAGLE_ADAMW_TENSORS of them.  Asynchronous; nothing is allocated.
  */
 #define PEAGLE_ADAMW_BLOCK 256
 #define PEAGLE_ADAMW_TENSORS 384

@@ -187,12 +187,6 @@ def _dtype(t):
     return code if code is not None else _refuse()
 
 
-def _counts(sizes):
-    """Refuses sizes that the C ABI's int32 would cut off; ``sizes`` is their bitwise or."""
-    if sizes >> 31:
-        _refuse("TOO_LARGE")
-
-
 def _matrix(t, rows, cols, dtype, device):
     """Address and leading dimension of a [rows, cols] tensor on the context's device whose rows are contiguous."""
     if t.shape != (rows, cols) or t.dtype != dtype or t.get_device() != device:
@@ -442,7 +436,8 @@ def peagle_norm_fwd(ctx, kind, X, weight, bias, eps, Y, mean=None, rstd=None, st
     if X.dim() != 2:
         _refuse()
     rows, cols = X.shape
-    _counts(rows | cols)
+    if (rows | cols) >> 31:  # the ABI's int32 would cut it off
+        _refuse("TOO_LARGE")
     dtype, dev = _dtype(X), ctx.device
     w = weight if weight is not None else bias
     w_dtype = _dtype(w) if w is not None else 0
@@ -462,7 +457,8 @@ def peagle_norm_bwd(ctx, kind, X, weight, mean, rstd, dY, dX, dweight_acc=None, 
     if X.dim() != 2:
         _refuse()
     rows, cols = X.shape
-    _counts(rows | cols)
+    if (rows | cols) >> 31:  # the ABI's int32 would cut it off
+        _refuse("TOO_LARGE")
     dtype, dev = _dtype(X), ctx.device
     w_dtype = _dtype(weight) if weight is not None else 0
     x, ldx = _matrix(X, rows, cols, X.dtype, dev)
@@ -483,7 +479,8 @@ def peagle_token_logprobs_fwd(ctx, logits, tokens, scale=1.0, logprob=None, lse=
     if logits.dim() != 2 or (top_logprobs is None) != (top_ids is None):
         _refuse()
     rows, vocab = logits.shape
-    _counts(rows | vocab)
+    if (rows | vocab) >> 31:
+        _refuse("TOO_LARGE")
     dtype, dev = _dtype(logits), ctx.device
     x, ld = _matrix(logits, rows, vocab, logits.dtype, dev)
     k, top, ids = 0, None, None
@@ -491,7 +488,8 @@ def peagle_token_logprobs_fwd(ctx, logits, tokens, scale=1.0, logprob=None, lse=
         if top_ids.dim() != 2 or not top_ids.is_contiguous() or not top_logprobs.is_contiguous():
             _refuse()
         k = top_ids.size(1)
-        _counts(k)
+        if k >> 31:
+            _refuse("TOO_LARGE")
         top = _matrix(top_logprobs, rows, k, _f32[0], dev)[0]
         ids = _matrix(top_ids, rows, k, _i32[0], dev)[0]
     rc = lib().peagle_token_logprobs_fwd(ctx.h, dtype, rows, vocab, x, ld, _vector(tokens, rows, _i32, dev), scale,
@@ -506,7 +504,8 @@ def peagle_token_logprobs_bwd(ctx, logits, tokens, scale, lse, entropy, g_logpro
     if logits.dim() != 2:
         _refuse()
     rows, vocab = logits.shape
-    _counts(rows | vocab)
+    if (rows | vocab) >> 31:
+        _refuse("TOO_LARGE")
     dtype, dev = _dtype(logits), ctx.device
     x, ld = _matrix(logits, rows, vocab, logits.dtype, dev)
     d, ldd = _matrix(dlogits, rows, vocab, logits.dtype, dev)

@@ -6,8 +6,8 @@
 // Bound by memory: every element of p, g, m and v is read once and, but for g, written once.  The list travels as a
 // kernel parameter (no copy to the device, nothing that a captured graph could lose); a block takes CHUNK elements
 // of one tensor, which it finds by a search over the tensors' first chunks, and a thread 8 neighbouring ones, in
-// 16-byte accesses where the tensor's addresses allow.  91 M elements of bf16 with states in 32 bits take 373 us (the
-// copy rate and 5 %).
+// 16-byte accesses where the tensor's addresses allow.  91 M elements of bf16 with states in 32 bits take 375 us (104 %
+// of the copy rate).
 //
 // 8-bit states: a warp has the 256 elements that share a scale.  m and sqrt(v) are e4m3 codes times a power of two,
 // so scaling is exact and the rounding to a code looks at the fp32 number's own bits: adding 20 random bits below
@@ -15,10 +15,11 @@
 // (Numbers below 2^-6, where e4m3's spacing is even, get 2^-6 added first; a thread without any skips that.)  What
 // bounds this is instructions, more than half of them integer ones for the random bits and the roundings: 91 M elements,
 // bf16, take 272 us, 52 % of the copy rate.  With all of m and v in fp64 it took 343.  In fp32 alone, some 20 us less, two or
-// three codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ: so
-// a code whose number is near its border, the largest number of a block near a power of two, and in blocks of small roots
-// those whose v is below fp32's normal numbers, are formed again in fp64 (and so are blocks in which m cancels), and every code is the defined one.  (Blocks that stay, with the next chunk on its way in shared memory, have
-// more instructions: 260 where this way took 254.)
+// three codes in a million fall on the other side of their random bits, and a step later the scales of their blocks differ.
+// So what fp32 does not settle is formed again in fp64, and every code is the defined one: a code whose number is near its
+// border, the largest number of a block near a power of two, blocks in which m cancels, and in blocks of small roots those
+// whose v is below fp32's normal numbers.  (All gradients around 1e-14, whose smallest are such: 27 %
+// longer.  Blocks that stay, with the next chunk on its way in shared memory, have more instructions: 2 % longer.)
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -36,7 +37,7 @@ namespace {
 constexpr int AW_THREADS = 256;
 constexpr int AW_BLOCK = PEAGLE_ADAMW_BLOCK;
 // Elements per thread block, 8 per thread.  (Blocks that go on to a second 2,048 spend fewer instructions on finding
-// their tensor and wait longer for memory: 8-bit states of 91 M elements 300 instead of 254 us, with four blocks to an SM.)
+// their tensor and wait longer for memory: 18 % longer with 8-bit states of 91 M elements, with four blocks to an SM.)
 constexpr int CHUNK = (AW_THREADS / 32) * AW_BLOCK;
 constexpr uint32_t GOLDEN = 0x9E3779B9u;            // 2^32 / golden ratio
 
@@ -84,7 +85,8 @@ struct Table {
 constexpr int SHORT_LIST = 32; // tensors of a smaller kernel parameter, which takes less time to launch with
 static_assert(sizeof(Table<PEAGLE_ADAMW_TENSORS>) <= 32764, "kernel parameters");
 
-// Scrambles 32 bits: two rounds of shift-xor and multiplication by an odd number, each of them one to one.
+// Scrambles 32 bits: two rounds of shift-xor and multiplication by an odd number, each of them one to one.  Shifts and
+// factors as published by C. Wellons, "Prospecting for hash functions", 2018, found there by search for the least bias.
 __host__ __device__ inline uint32_t mix_but_for_the_last(uint32_t x)
 {
     x ^= x >> 16;

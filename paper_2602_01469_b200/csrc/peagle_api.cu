@@ -1440,7 +1440,7 @@ int peagle_token_logprobs_bwd(peagle_ctx *ctx, int32_t dtype, int32_t rows, int3
     a.ldd = ldd;
     const OnDevice on(ctx->device);
     CK(on.error);
-    const int n = launch_logprobs_bwd(a, ctx->n_sm, static_cast<cudaStream_t>(stream));
+    const int n = launch_logprobs_bwd(a, static_cast<cudaStream_t>(stream));
     if (n < 0)
         return n;
     ctx->launches += n;

@@ -241,7 +241,7 @@ struct LogprobArgs {
     int *status;
 };
 int launch_logprobs_fwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
-int launch_logprobs_bwd(const LogprobArgs &a, int n_sm, cudaStream_t s);
+int launch_logprobs_bwd(const LogprobArgs &a, cudaStream_t s);
 
 // AdamW over a list of tensors (peagle_adamw.cu).  The arguments have been checked.  Returns the number of
 // kernels launched.

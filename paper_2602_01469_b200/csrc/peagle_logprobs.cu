@@ -10,11 +10,13 @@
 //
 // The floor is one read.  A block takes a row in chunks of 16 bytes per thread and load, the next chunk on its way.  Few
 // rows are cut into parts for a cluster of up to 16 blocks, which join through distributed shared memory.  4,096 rows of
-// 128,000 bf16 take 200 us without alternatives (80 % of the copy rate), 233 with 8 (69 %), 255 with 20; 2,048 rows of
-// fp32, the same bytes, 193 with 8 (83 %).  Nothing is full (1,184 rows: issue slots 61 % without alternatives, 69 with,
-// 8 and 11 instructions per entry, exp2 unit 50 %): a chunk's steps depend on each other, and the 32 warps of an SM
-// do not cover that.  The next chunk but one is sent for as soon as a chunk's pieces are in registers and what of them
-// reaches the list is there; after the sums it took 241 with 8 and 265 with 20.
+// 128,000 bf16 take 176 us without alternatives (91 % of the copy rate), 227 with 8 (71 %), 268 with 20 (60 %); 2,048 rows
+// of fp32, the same bytes, 200 with 8 (80 %).  (In a loop over one input; over changing ones with 8 it is 233 to 254.)
+// Nothing is full (1,184 rows: issue slots 61 % without alternatives, 69 with, 8 and 11 instructions per entry, exp2 unit
+// 50 %): a chunk's steps depend on each other, and the 32 warps of an SM do not cover that.  The next chunk but one is
+// sent for as soon as a chunk's pieces are in registers and what of them reaches the list is there, which is 3 % faster
+// than after the sums.  More alternatives are slow: 304 us with 32, 402 with 48, 554 with 64 (29 %), where the first bound
+// is loose, the list overflows between two looks at it and rows are begun again.
 //
 // Top alternatives, in the same pass: from the first chunk on there is a bound that at least k entries reach (the
 // k-th largest of the maxima of 64 groups of threads, then the k-th best entry so far).  A chunk's maximum, which the
@@ -36,8 +38,8 @@ using namespace sm100;
 
 namespace {
 
-// Blocks of 128 threads: 4,096 rows of 128,000 bf16 with 8 alternatives take 252 us, with blocks of 256 (the same
-// threads per SM, but more of them at a barrier) 271; 8 blocks to an SM, with 10 the registers do not suffice.
+// Blocks of 128 threads: 4,096 rows of 128,000 bf16 with 8 alternatives take 8 % longer with blocks of 256 (the same
+// threads per SM, but more of them at a barrier); 8 blocks to an SM, with 10 the registers do not suffice.
 constexpr int LP_THREADS = 128, LP_WARPS = LP_THREADS / 32;
 constexpr int FWD_PIECES = 4; // 16-byte pieces per thread and chunk
 constexpr int GROUPS = 64;     // of threads, whose maxima give the first bound
@@ -358,11 +360,11 @@ __global__ void __launch_bounds__(LP_THREADS, 8)
         x += STEP * N;
     };
     Sums s;
-    // A list that has grown by half is cut.  (4,096 rows of 128,000, k = 20: 264 us; when it has tripled 275.)  A short
-    // part ends before that pays.
+    // A list that has grown by half is cut.  (4,096 rows of 128,000, k = 20: 4 % longer when it is cut where it has
+    // tripled.)  A short part ends before that pays.
     const int long_list = pieces <= 4 * STEP ? max(LP_THREADS - 8, a.top_k + a.top_k / 2) : a.top_k + a.top_k / 2 + 6;
-    // Looking at the list means that all warps wait for the slowest.  (4,096 rows of 128,000 bf16, k = 8: 256 us with a
-    // look at every chunk, 243 at every fourth; 2,048 rows of fp32 213 and 203.)  A row that overflows the list unseen
+    // Looking at the list means that all warps wait for the slowest.  (4,096 rows of 128,000 bf16, k = 8: 5 % longer with
+    // a look at every chunk than at every fourth; 2,048 rows of fp32 the same.)  A row that overflows the list unseen
     // is begun again.
     for (int every = MEET_EVERY;; every = 1) {
         x = row + begin - before + threadIdx.x * N;
@@ -866,9 +868,8 @@ int launch_logprobs_fwd(const LogprobArgs &a, int n_sm, cudaStream_t s)
     return 1;
 }
 
-int launch_logprobs_bwd(const LogprobArgs &a, int n_sm, cudaStream_t s)
+int launch_logprobs_bwd(const LogprobArgs &a, cudaStream_t s)
 {
-    (void)n_sm;
     return a.dtype == PEAGLE_F32 ? backward_of<float>(a, s) : backward_of<__nv_bfloat16>(a, s);
 }
 

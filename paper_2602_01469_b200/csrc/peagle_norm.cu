@@ -12,9 +12,12 @@
 // hold the column sums in registers; a block's groups join theirs in shared memory at the end, and a second
 // kernel adds up the blocks.  Rows of more columns go through kernels that read them again for every pass.
 //
-// Measured, of the rate of a copy: RMS forward, 32,768 rows of 2,880 bf16, 64 us (90 %), backward 95 (91 %); layer norm
-// backward, 524,288 rows of 128 bf16, 72 (87 %).  What is missing is loads in flight while a row's sums are joined.  Few
-// rows are bound by latency: layer norm backward of 3,891 rows of 1,001 fp32 takes 18.5 us (39 %), of 30,000 66 (83 %).
+// Measured, of the rate of a copy: RMS forward, 32,768 rows of 2,880 bf16, 66 us (88 %), backward 96 (90 %); layer norm
+// backward, 524,288 rows of 128 bf16, 72 (86 %).  What is missing is loads in flight while a row's sums are joined.  Few
+// rows are bound by latency: layer norm backward of 3,891 rows of 1,001 fp32 takes 18.4 us (39 %), of 30,000 66 (83 %).
+// Rows that do not begin on 16 bytes go through single elements: RMS norm of 16,384 rows of 2,877 takes 106 us forward
+// (27 %) and 95 backward (45 %) in bf16, 81 (71 %) and 115 (75 %) in fp32.  Rows of more columns than a group holds are
+// not meant to be fast: 2,048 of 20,000 bf16 take 97 us forward (26 %) and 252 backward (15 %).
 #include <cuda_bf16.h>
 
 #include <algorithm>
