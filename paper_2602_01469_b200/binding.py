@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from bisect import bisect_left
 
 import numpy as np
 
@@ -250,7 +251,8 @@ class AdamWTensors:
     """The tensors of ``peagle_adamw_step``, put together once: owns the array a call passes and keeps the tensors
     alive.  Each item is a dict of ``param``, ``grad``, ``m``, ``v`` and, where they apply, ``master`` (fp32, for bf16
     parameters), ``m_scale`` and ``v_scale`` (states in 8 bits: m and v are float8_e4m3fn, a scale for every
-    ADAMW_BLOCK elements), ``weight_decay``.  Contiguous device tensors; no two may share memory."""
+    ADAMW_BLOCK elements), ``weight_decay``.  Contiguous device tensors; no two may share memory, but for gradients
+    among themselves."""
 
     def __init__(self, items):
         import torch
@@ -287,6 +289,7 @@ class AdamWTensors:
         written.sort()
         if any(end > begin for (_, end), (begin, _) in zip(written, written[1:])):
             _refuse("BAD_RANGE")
+        self._begins, self._ends = [begin for begin, _ in written], [end for _, end in written]
         self.set_grads([i["grad"] for i in self.items])
 
     def set_grads(self, grads):
@@ -298,7 +301,11 @@ class AdamWTensors:
         for c, g in zip(self.c, grads):
             if g.get_device() != self.device or g.numel() != c.count or not g.is_contiguous():
                 _refuse()
-            fresh.append((g.data_ptr(), _dtype(g)))
+            at, code = g.data_ptr(), _dtype(g)
+            before = bisect_left(self._begins, at + (2 if code else 4) * c.count) - 1
+            if c.count and before >= 0 and self._ends[before] > at:
+                _refuse("BAD_RANGE")
+            fresh.append((at, code))
         for c, i, g, (at, code) in zip(self.c, self.items, grads, fresh):
             c.grad, c.grad_dtype, i["grad"] = at, code, g
 

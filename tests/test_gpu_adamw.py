@@ -446,3 +446,23 @@ def test_refused_gradients_leave_the_old_ones(ctx):
     torch.cuda.synchronize()
     for k, (b, a) in enumerate(zip(before, tensors.items)):
         check(b, a, k, 1, 0)
+
+
+def test_gradients_in_the_memory_of_what_is_written_are_refused(ctx):
+    """The step reads a gradient more than once, and what it writes in between must not be in its place."""
+    item = {"param": torch.zeros(300, device=DEV), "m": torch.zeros(300, device=DEV), "v": torch.zeros(300, device=DEV)}
+    around = torch.zeros(1000, device=DEV)
+    item["param"] = around[300:600]
+    fine = [around[:300], around[600:900], torch.zeros(300, device=DEV)]
+    for g in fine:
+        tensors = binding.AdamWTensors([{**item, "grad": g}])
+    for g in (item["param"], item["m"], item["v"], around[1:301], around[599:899], around[450:750],
+              around[400:550].view(torch.uint8).view(BF16), around[599:749].view(torch.uint8).view(BF16)):
+        for call in (lambda: binding.AdamWTensors([{**item, "grad": g}]), lambda: tensors.set_grads([g])):
+            with pytest.raises(binding.PeagleError) as e:
+                call()
+            assert e.value.status == binding.STATUS["BAD_RANGE"]
+    two = [{**item, "grad": fine[0]}, {"param": around[:0], "m": around[:0], "v": around[:0], "grad": item["param"][:0]}]
+    binding.AdamWTensors(two)                                        # nothing of a tensor without elements is written
+    other = {k: torch.zeros(300, device=DEV) for k in ("param", "m", "v")}
+    binding.AdamWTensors([{**item, "grad": fine[2]}, {**other, "grad": fine[2]}])   # read twice
