@@ -291,6 +291,29 @@ def test_tiny_roots_are_kept_in_8_bits(ctx, dtype, empty):
         check(b, item, 0, step, 5, how)
 
 
+@pytest.mark.parametrize("count", [20, 60])
+@pytest.mark.parametrize("eps", [1e-20, 1e-12])
+def test_tiny_roots_among_tensors_of_all_kinds(ctx, count, eps):
+    """Short and long lists, states in 8 bits alone and beside others, an eps below what fp32 settles and one above."""
+    gen = torch.Generator().manual_seed(23)
+    how = dict(lr=3e-3, beta1=0.9, beta2=0.98, eps=eps)
+    kinds8 = [k for k in KINDS if k[2] == 8]
+    for kinds in (kinds8, kinds8 + [(F32, F32, 32, False)]):
+        items = [make(gen, 1 + (i * 97) % 1500, *kinds[i % len(kinds)], 0.1, offset=i % 5) for i in range(count)]
+        for i in items:
+            if i["m"].dtype == F8:
+                i["grad"].copy_(tiny_gradients(gen, i["grad"].numel()))
+                i["v"].view(torch.uint8)[::3] = 0
+                i["m"].view(torch.uint8)[::3] = 0
+        tensors = binding.AdamWTensors(items)
+        for step in (1, 2):
+            before = [snapshot(i) for i in items]
+            binding.peagle_adamw_step(ctx, tensors, step=step, seed=8, **how)
+            torch.cuda.synchronize()
+            for k, (b, a) in enumerate(zip(before, items)):
+                check(b, a, k, step, 8, how)
+
+
 @pytest.mark.parametrize("eps", [2.0 ** -126, 1e-30, 1e-20, 1e-8])
 def test_tiny_roots_divide_the_step_in_32_bits(ctx, eps):
     """The step from the m and v that are stored, which are fp32's, some of them no normal numbers."""
